@@ -16,7 +16,8 @@ LIB_PATH = os.path.join(_HERE, "libodma.so")
 
 def sources():
     src = sorted(glob.glob(os.path.join(_HERE, "csrc", "*.cu")) + glob.glob(os.path.join(_HERE, "csrc", "*.cpp")))
-    hdr = sorted(glob.glob(os.path.join(_HERE, "csrc", "*.hpp")) + [os.path.join(_ROOT, "include", "odma.h")])
+    hdr = sorted(glob.glob(os.path.join(_HERE, "csrc", "*.hpp")) + glob.glob(os.path.join(_HERE, "csrc", "*.cuh")) +
+                 [os.path.join(_ROOT, "include", "odma.h")])
     return src, hdr
 
 
