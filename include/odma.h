@@ -180,7 +180,7 @@ typedef struct odma_tables {
     int32_t off_base, off_cap, off_len, off_cu_new, off_cta, off_items, off_combine;
     int32_t tile_tokens;
     int32_t one_new_each; /* 1 when every request appends exactly one token (decode step) */
-    int32_t reserved;
+    int32_t reserved;     /* 1: built on the device (odma_build_tables_device) */
     int64_t kv_tokens; /* sum of len */
     uint64_t epoch;
 } odma_tables;
@@ -277,6 +277,48 @@ int32_t odma_plan_host(odma_pool* pool, const uint64_t* reqs, const int32_t* n_n
 int32_t odma_build_tables(odma_pool* pool, const uint64_t* reqs, const int32_t* n_new, int32_t n,
                           void* d_table, uint64_t table_bytes, void* stream, odma_tables* out);
 
+/* ---- the same tables built on the GPU -----------------------------------------------------
+ * For a decode loop whose lengths live in device memory (a captured graph, a sampler that ends
+ * requests on the device): one kernel, no host planning, no copy.
+ * odma_slab_table writes the slabs of n live requests to d_slabs (device, [n][2] int32: base,
+ * capacity; 8-byte aligned) and, unless d_len is NULL, their committed lengths to d_len (device,
+ * [n]), with asynchronous copies; to be repeated when the batch or a slab changes.
+ * odma_build_tables_device reads d_slabs, d_len (tokens before the step) and d_n_new ([n], tokens
+ * of the step; NULL: one each, n_new_total = n) and writes
+ *   d_table      the table described at odma_tables (16-byte aligned, table_bytes >=
+ *                odma_tables_bytes(pool, n))
+ *   d_len_next   [n] tokens after the step, or NULL; may be d_len itself, so that replays of a
+ *                captured step walk on by themselves
+ *   d_slots      [n_new_total] or NULL: the slot map.  The row of KV head 0 inside one K (or V)
+ *                array that each new token takes, tokens in request order (head h of slab {base, cap}:
+ *                + h*cap); -1 for a row that no request has
+ *   d_positions  [n_new_total] or NULL: the token's position in its slab, or -1
+ * n_new_total is the number of rows the step's buffers have; the tokens of d_n_new may be fewer.
+ * The descriptor's counts are bounds that hold for any lengths (n_items = n*kv_heads + n_ctas,
+ * n_ctas = plan_ctas, n_combine = min(n*kv_heads, n_ctas)); items in excess have request -1, combine
+ * records in excess n_slots 0, empty CTA records an empty range; reserved = 1.  kv_tokens is 0 (not known).
+ * A request with no token after the step has no item and leaves its rows of `out` and `lse` as they
+ * were (behind a prefix: the prefix alone, see below).
+ * Plan: the streams in order, t tiles of 64 tokens costing t + 1; share c begins at cost c*C, C = max(4,
+ * ceil(cost / n_ctas)); a cut closer than 3 tiles to an end of its stream moves to that end, a stream
+ * shorter than 6 tiles is not cut.
+ * A request that breaks base % 16 = 0, 0 <= base, base + cap <= T, 0 <= len, 0 <= n_new, len + n_new <=
+ * cap, or whose rows pass n_new_total, is refused: base, cap and len words 0, no item, its rows of the
+ * slot map -1, its length not advanced, nothing appended for it; odma_check_status then returns
+ * ODMA_ERR_OVERFLOW.  (n_new outside [0, n_new_total] counts as 0 rows.)  That two slabs do not
+ * overlap is not checked.
+ * The host's lengths do not follow: commit them with odma_commit_step before the next call that uses
+ * them (odma_ensure_capacity, odma_free, host-built tables).  n at most 4096 and plan_ctas at most 1024.
+ * May be captured; so may odma_append_kv, odma_append_qkv, odma_decode_attention and
+ * odma_decode_attention_prefix with the descriptor (odma_decode_attention_static too).  Two captured
+ * steps of one pool share its scratch like any two calls: one stream, or ordered by the caller. */
+int32_t odma_slab_table(odma_pool* pool, const uint64_t* reqs, int32_t n, int32_t* d_slabs, int32_t* d_len,
+                        void* stream);
+int32_t odma_build_tables_device(odma_pool* pool, const int32_t* d_slabs, const int32_t* d_len,
+                                 const int32_t* d_n_new, int32_t n, int32_t n_new_total, void* d_table,
+                                 uint64_t table_bytes, int32_t* d_len_next, int32_t* d_slots,
+                                 int32_t* d_positions, void* stream, odma_tables* out);
+
 /* ---- chunked prefill over the slabs (Section II-A: the prefill phase fills the cache with the
  *      prompt's keys and values before decoding starts) --------------------------------------
  * A chunk of n_new[i] >= 1 prompt tokens per request is appended with the ordinary calls
@@ -301,6 +343,41 @@ int32_t odma_build_prefill_tables(odma_pool* pool, const uint64_t* reqs, const i
 int32_t odma_append_kv(odma_pool* pool, int32_t layer, const odma_tables* tables,
                        const void* k_new, const void* v_new, void* stream);
 
+/* ---- norm, rotation and append in one pass --------------------------------------------------
+ * What lies between a layer's projections and its attention: for every new token, every query and
+ * key head x of D = head_dim elements
+ *   y = x / sqrt(mean(x^2) + eps) * w          with w = q_norm or k_norm; y = x where that is NULL
+ *   z_a = y_a cos t - y_b sin t,  z_b = y_b cos t + y_a sin t,   t = position[axis(i)] * inv_freq[i]
+ * for the pairs i < rot_dim/2, (a, b) = (i, i + rot_dim/2), or (2i, 2i+1) when `interleaved`; the other
+ * elements are z = y.  z of the queries goes to q_out, z of the keys and the values as they are go
+ * to the slab rows that odma_append_kv would write.  Arithmetic is fp32 (the angle fp64), with one
+ * rounding, to the io type or, for an 8-bit pool, of fp32 z * (1.0f / scale) to the nearest code.
+ * Several axes (time, height, width): the first section[0] pairs turn by the first row of positions,
+ * the next section[1] by the second, and so on; the sections add up to rot_dim/2. */
+typedef struct odma_qkv_prep {
+    const void* q_norm;       /* device, [head_dim] in the pool's io type, 16-byte aligned, or NULL */
+    const void* k_norm;
+    const float* inv_freq;    /* device, [rot_dim/2] */
+    const int32_t* positions; /* device, n_axes rows of n_new_total; NULL: the token's position in its slab */
+    int64_t q_stride;         /* elements from one token to the next in q, k_new, v_new (so that they may be */
+    int64_t k_stride;         /* cut out of one projection's output): multiples of 16 bytes; 0 = packed */
+    int64_t v_stride;
+    int64_t pos_stride;       /* elements from one axis to the next in positions; 0 = n_new_total */
+    int32_t rot_dim;          /* multiple of 8 in [0, head_dim]; 0: no rotation */
+    int32_t interleaved;      /* 0 or 1 */
+    int32_t n_axes;           /* 1 .. 4 */
+    int32_t section[4];       /* pairs per axis (n_axes = 1: not read) */
+    float eps;                /* finite, >= 0 */
+} odma_qkv_prep;
+/* q: device, [n_new_total, q_heads, D]; k_new, v_new: device, [n_new_total, kv_heads, D], in the pool's io
+ * type, 16-byte aligned, heads of a token packed, tokens a stride apart.  q_out: device, packed
+ * [n_new_total, q_heads, D], ready for odma_decode_attention; it may be q itself when q is packed, and
+ * must not overlap the inputs otherwise.  tables: host- or device-built.  Rows of q_out that belong to
+ * no request (or a refused one) are left as they were.  head_dim a multiple of 8, at most 256. */
+int32_t odma_append_qkv(odma_pool* pool, int32_t layer, const odma_tables* tables, const void* q,
+                        const void* k_new, const void* v_new, void* q_out, int32_t q_heads,
+                        const odma_qkv_prep* prep, void* stream);
+
 /* ---- decode attention over the slabs (the bandwidth consumer, Sections III-A and V-B) ---
  * out[i][h] = softmax_j(q[i][h] . K_i[h div g][j] / sqrt(head_dim)) V_i[h div g], j < len[i],
  * g = q_heads / kv_heads (K_i, V_i of an 8-bit pool: the dequantised values).  q, out: device,
@@ -309,6 +386,26 @@ int32_t odma_append_kv(odma_pool* pool, int32_t layer, const odma_tables* tables
  * stream was split, the combine kernel. */
 int32_t odma_decode_attention(odma_pool* pool, int32_t layer, const void* q, int32_t q_heads,
                               const odma_tables* tables, void* out, float* lse, void* stream);
+
+/* ---- decode attention of a batch that shares a prefix ----------------------------------------
+ * The batch's requests begin with the same prefix_len tokens (a system prompt, a document), held once,
+ * in the slab of the live request `prefix_req`; the slabs of `tables` hold what follows.  With K_P, V_P
+ * the first prefix_len tokens of that slab,
+ *   out[i][h] = softmax_j(q[i][h] . [K_P ; K_i][j] / sqrt(head_dim)) [V_P ; V_i],   lse likewise.
+ * The prefix's part is computed for the whole batch at once, its keys and values read once per 256
+ * query rows of a KV head instead of once per request.  prefix_len may be 0 .. the prefix's committed
+ * length (ODMA_ERR_OVERFLOW beyond); a request of a device-built table without a token of its own
+ * gets the prefix alone (with prefix_len 0: zeros and an lse of -inf).  Arguments otherwise as for
+ * odma_decode_attention; head_dim 32, 64 or 128.
+ * workspace: device, 256-byte aligned, the caller's: partial results of the prefix's splits (and, for an
+ * 8-bit pool, the prefix as bf16).  odma_prefix_workspace_bytes gives the size for n requests at the
+ * best number of splits (0 for a bad shape); with less, down to one split, the call uses fewer.
+ * Calls that overlap on the GPU need workspaces of their own. */
+uint64_t odma_prefix_workspace_bytes(const odma_pool* pool, int32_t q_heads, int32_t n, int32_t prefix_len);
+int32_t odma_decode_attention_prefix(odma_pool* pool, int32_t layer, const void* q, int32_t q_heads,
+                                     uint64_t prefix_req, int32_t prefix_len, const odma_tables* tables,
+                                     void* workspace, uint64_t workspace_bytes, void* out, float* lse,
+                                     void* stream);
 
 /* One decode step of one layer from HOST buffers: builds the tables for reqs (one new token
  * each), takes h_q [n,q_heads,head_dim], h_k_new, h_v_new [n,kv_heads,head_dim], appends,
@@ -371,7 +468,8 @@ int32_t odma_decode_attention_static(const odma_pool* pool, const void* dev_base
                                      void* out, float* lse, void* stream);
 
 /* Synchronises `stream` and returns the device status word as an error code (ODMA_OK,
- * ODMA_ERR_TIMEOUT, or ODMA_ERR_CUDA for a failed stream), clearing it. */
+ * ODMA_ERR_TIMEOUT, ODMA_ERR_OVERFLOW for a request that odma_build_tables_device refused, or
+ * ODMA_ERR_CUDA for a failed stream), clearing it. */
 int32_t odma_check_status(odma_pool* pool, void* stream);
 
 /* Failure detection, exercised without a fault: launches a one-thread kernel whose only wait

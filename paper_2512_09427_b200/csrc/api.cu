@@ -307,6 +307,9 @@ int32_t check_tables(const odma_pool* pool, const odma_tables* t) {
     return ODMA_OK;
 }
 
+// The table is written by a kernel (odma_build_tables_device); its counts in the descriptor are bounds.
+bool built_on_device(const odma_tables* t) { return t->reserved != 0; }
+
 void fill_decode_params(const odma_pool* pool, int32_t layer, const void* q, int32_t q_heads,
                         const odma_tables* t, void* out, float* lse, DecodeParams* p) {
     const int32_t* tab = static_cast<const int32_t*>(t->d_table);
@@ -340,6 +343,7 @@ void fill_decode_params(const odma_pool* pool, int32_t layer, const void* q, int
     p->chained = 0;
     p->early_ok = 0;
     p->n_layers = 1;
+    p->partial_only = 0;
     p->kv_fp8 = pool->dtype == ODMA_DTYPE_FP8_E4M3 ? 1 : 0;
     p->k_scale = p->v_scale = p->k_inv = p->v_inv = 1.f;
     if (p->kv_fp8) {
@@ -715,6 +719,165 @@ int32_t odma_append_kv(odma_pool* pool, int32_t layer, const odma_tables* tables
     return launch_append(ap, as_stream(stream)) == cudaSuccess ? ODMA_OK : ODMA_ERR_CUDA;
 }
 
+int32_t odma_slab_table(odma_pool* pool, const uint64_t* reqs, int32_t n, int32_t* d_slabs, int32_t* d_len, void* stream) {
+    if (!pool || !pool->dev_base || !reqs || !d_slabs || n < 1 || n > pool->alloc.config().max_batch) return ODMA_ERR_INVALID;
+    if ((reinterpret_cast<uintptr_t>(d_slabs) & 7u) != 0 || (reinterpret_cast<uintptr_t>(d_len) & 3u) != 0) return ODMA_ERR_INVALID;
+    for (int32_t i = 0; i < n; ++i)
+        if (!pool->alloc.find(reqs[i])) return ODMA_ERR_UNKNOWN_REQ;
+    Staging& st = pool->staging[pool->staging_next];
+    pool->staging_next = (pool->staging_next + 1) % kStagingSlots;
+    if (st.in_flight && cudaEventSynchronize(st.done) != cudaSuccess) return ODMA_ERR_CUDA;
+    st.in_flight = false;
+    for (int32_t i = 0; i < n; ++i) {            // 3n words; a staging slot holds the largest table
+        const Request* r = pool->alloc.find(reqs[i]);
+        st.host[2 * i] = static_cast<int32_t>(r->base);
+        st.host[2 * i + 1] = static_cast<int32_t>(r->cap);
+        st.host[2 * n + i] = static_cast<int32_t>(r->len);
+    }
+    const size_t word = sizeof(int32_t), count = static_cast<size_t>(n);
+    if (cudaMemcpyAsync(d_slabs, st.host, 2 * count * word, cudaMemcpyHostToDevice, as_stream(stream)) != cudaSuccess ||
+        (d_len && cudaMemcpyAsync(d_len, st.host + 2 * n, count * word, cudaMemcpyHostToDevice, as_stream(stream)) != cudaSuccess) ||
+        cudaEventRecord(st.done, as_stream(stream)) != cudaSuccess)
+        return ODMA_ERR_CUDA;
+    st.in_flight = true;
+    return ODMA_OK;
+}
+
+int32_t odma_build_tables_device(odma_pool* pool, const int32_t* d_slabs, const int32_t* d_len, const int32_t* d_n_new,
+                                 int32_t n, int32_t n_new_total, void* d_table, uint64_t table_bytes, int32_t* d_len_next,
+                                 int32_t* d_slots, int32_t* d_positions, void* stream, odma_tables* out) {
+    if (!pool || !pool->dev_base || !d_slabs || !d_len || !d_table || !out || n < 1 || n_new_total < 0) return ODMA_ERR_INVALID;
+    if (n > pool->alloc.config().max_batch || n > kMaxDeviceBatch || pool->plan_ctas > kMaxDeviceCtas) return ODMA_ERR_INVALID;
+    if (!d_n_new && n_new_total != n) return ODMA_ERR_INVALID;
+    if (!aligned16(d_table) || (reinterpret_cast<uintptr_t>(d_slabs) & 7u) != 0 || table_bytes < odma_tables_bytes(pool, n))
+        return ODMA_ERR_INVALID;
+    for (const void* w : {static_cast<const void*>(d_len), static_cast<const void*>(d_n_new), static_cast<const void*>(d_len_next),
+                          static_cast<const void*>(d_slots), static_cast<const void*>(d_positions)})
+        if ((reinterpret_cast<uintptr_t>(w) & 3u) != 0) return ODMA_ERR_INVALID;
+    auto up4 = [](int32_t w) { return (w + 3) & ~3; };
+    const int32_t streams = n * pool->kv_heads, ctas = pool->plan_ctas;
+    odma_tables t{};
+    t.d_table = d_table;
+    t.n = n;
+    t.n_new_total = n_new_total;
+    t.n_items = streams + ctas;
+    t.n_ctas = ctas;
+    t.n_combine = std::min(streams, ctas);
+    t.off_base = 0;
+    t.off_cap = up4(n);
+    t.off_len = 2 * up4(n);
+    t.off_cu_new = 3 * up4(n);
+    t.off_cta = t.off_cu_new + up4(n + 1);
+    t.off_items = t.off_cta + kCtaWords * ctas;
+    t.off_combine = t.off_items + 8 * t.n_items;
+    t.words = t.off_combine + 4 * t.n_combine;
+    t.tile_tokens = kTileTokens;
+    t.one_new_each = d_n_new ? 0 : 1;
+    t.reserved = 1;                              // built_on_device
+    t.kv_tokens = 0;
+    t.epoch = pool->alloc.epoch();
+    DeviceTablesParams p;
+    p.slabs = d_slabs;
+    p.len = d_len;
+    p.n_new = d_n_new;
+    p.len_next = d_len_next;
+    p.slots = d_slots;
+    p.positions = d_positions;
+    p.table = static_cast<int32_t*>(d_table);
+    p.status = pool->d_status;
+    p.tokens = pool->alloc.T();
+    p.n = n;
+    p.kv_heads = pool->kv_heads;
+    p.n_ctas = ctas;
+    p.n_new_total = n_new_total;
+    p.n_items = t.n_items;
+    p.n_combine = t.n_combine;
+    p.off_base = t.off_base;
+    p.off_cap = t.off_cap;
+    p.off_len = t.off_len;
+    p.off_cu_new = t.off_cu_new;
+    p.off_cta = t.off_cta;
+    p.off_items = t.off_items;
+    p.off_combine = t.off_combine;
+    pool->decode_was_last = false;
+    pool->last_fused_tensor = false;
+    if (launch_build_tables(p, as_stream(stream)) != cudaSuccess) return ODMA_ERR_CUDA;
+    *out = t;
+    return ODMA_OK;
+}
+
+int32_t odma_append_qkv(odma_pool* pool, int32_t layer, const odma_tables* tables, const void* q, const void* k_new,
+                        const void* v_new, void* q_out, int32_t q_heads, const odma_qkv_prep* prep, void* stream) {
+    if (!pool || !pool->dev_base || layer < 0 || layer >= pool->layers || !prep) return ODMA_ERR_INVALID;
+    if (!tables || !tables->d_table || tables->n < 1 || tables->n_new_total < 0) return ODMA_ERR_INVALID;
+    const int32_t D = pool->head_dim, pairs = prep->rot_dim / 2;
+    if (q_heads < pool->kv_heads || q_heads % pool->kv_heads != 0) return ODMA_ERR_INVALID;
+    if (D % 8 != 0 || D > 2 * kMaxRotPairs || prep->rot_dim < 0 || prep->rot_dim > D || prep->rot_dim % 8 != 0) return ODMA_ERR_INVALID;
+    if (pairs > 0 && (!prep->inv_freq || prep->n_axes < 1 || prep->n_axes > kMaxAxes)) return ODMA_ERR_INVALID;
+    if (prep->interleaved != 0 && prep->interleaved != 1) return ODMA_ERR_INVALID;
+    if ((prep->q_norm || prep->k_norm) && !(prep->eps >= 0.f && std::isfinite(prep->eps))) return ODMA_ERR_INVALID;
+    QkvParams p;
+    int32_t end = 0;
+    for (int32_t a = 0; a < kMaxAxes; ++a) {
+        if (a < prep->n_axes && prep->n_axes > 1) {
+            if (prep->section[a] < 0) return ODMA_ERR_INVALID;
+            end = prep->section[a] > pairs - end ? pairs + 1 : end + prep->section[a];
+            if (end > pairs) return ODMA_ERR_INVALID;
+        } else {
+            end = prep->n_axes > 1 ? end : pairs;
+        }
+        p.section_end[a] = end;
+    }
+    if (pairs > 0 && end != pairs) return ODMA_ERR_INVALID;
+    const int64_t packed_q = static_cast<int64_t>(q_heads) * D, packed_kv = static_cast<int64_t>(pool->kv_heads) * D;
+    p.q_stride = prep->q_stride ? prep->q_stride : packed_q;
+    p.k_stride = prep->k_stride ? prep->k_stride : packed_kv;
+    p.v_stride = prep->v_stride ? prep->v_stride : packed_kv;
+    p.pos_stride = prep->pos_stride ? prep->pos_stride : tables->n_new_total;
+    if (p.q_stride < packed_q || p.k_stride < packed_kv || p.v_stride < packed_kv || p.pos_stride < tables->n_new_total)
+        return ODMA_ERR_INVALID;
+    if (p.q_stride * pool->io_bytes % 16 != 0 || p.k_stride * pool->io_bytes % 16 != 0 || p.v_stride * pool->io_bytes % 16 != 0)
+        return ODMA_ERR_INVALID;
+    if (tables->n_new_total == 0) return ODMA_OK;
+    if (!q || !k_new || !v_new || !q_out || !aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(q_out) ||
+        !aligned16(prep->q_norm) || !aligned16(prep->k_norm) || (reinterpret_cast<uintptr_t>(prep->inv_freq) & 3u) != 0 ||
+        (reinterpret_cast<uintptr_t>(prep->positions) & 3u) != 0)
+        return ODMA_ERR_INVALID;
+    const int32_t* tab = static_cast<const int32_t*>(tables->d_table);
+    p.base = tab + tables->off_base;
+    p.cap = tab + tables->off_cap;
+    p.len = tab + tables->off_len;
+    p.cu_new = tab + tables->off_cu_new;
+    p.pool = pool->dev_base;
+    p.q = q;
+    p.k_new = k_new;
+    p.v_new = v_new;
+    p.q_out = q_out;
+    p.q_norm = prep->q_norm;
+    p.k_norm = prep->k_norm;
+    p.inv_freq = prep->inv_freq;
+    p.positions = prep->positions;
+    p.rows_per_array = pool->rows_per_array;
+    p.layer = layer;
+    p.n = tables->n;
+    p.q_heads = q_heads;
+    p.kv_heads = pool->kv_heads;
+    p.head_dim = D;
+    p.n_new_total = tables->n_new_total;
+    p.one_new_each = tables->one_new_each;
+    p.quantize = pool->dtype == ODMA_DTYPE_FP8_E4M3 ? 1 : 0;
+    p.rot_pairs = pairs;
+    p.interleaved = prep->interleaved;
+    p.n_axes = prep->n_axes;
+    p.eps = prep->eps;
+    p.k_inv = p.quantize ? 1.0f / pool->k_scale[layer] : 1.f;
+    p.v_inv = p.quantize ? 1.0f / pool->v_scale[layer] : 1.f;
+    pool->decode_was_last = false;
+    pool->last_fused_tensor = false;
+    ProfScope ps(pool, ODMA_K_APPEND, as_stream(stream));
+    return launch_append_qkv(p, pool->io_dtype == ODMA_DTYPE_F32, as_stream(stream)) == cudaSuccess ? ODMA_OK : ODMA_ERR_CUDA;
+}
+
 }  // extern "C"
 
 namespace {
@@ -753,11 +916,13 @@ cudaError_t launch_tensor_decode(const odma_pool* pool, const TensorMaps& maps, 
     const int32_t want = pool->alloc.config().readout;
     bool defer = want == ODMA_READOUT_LATE;
     if (want == ODMA_READOUT_AUTO)
-        defer = static_cast<int64_t>(p.n_layers) * t->n_items >= kLateItemsPerCta * n_ctas &&
+        defer = !built_on_device(t) && static_cast<int64_t>(p.n_layers) * t->n_items >= kLateItemsPerCta * n_ctas &&
                 t->kv_tokens * pool->kv_heads <= kLateTokensPerItem * t->n_items;
     defer = defer && mode == kModeSlab && !p.kv_fp8;
-    return umma ? launch_decode_umma(maps, p, mode, n_ctas, stream, lens, span, defer)
-                : launch_decode_tc(maps, p, mode, n_ctas, stream, lens);
+    // the kernels read their plan before they wait for the kernel ahead, which may be the one that writes it
+    const bool overlap = !built_on_device(t);
+    return umma ? launch_decode_umma(maps, p, mode, n_ctas, stream, lens, span, defer, overlap)
+                : launch_decode_tc(maps, p, mode, n_ctas, stream, lens, overlap);
 }
 
 // odma_decode_attention; with k_new / v_new the tensor-core kernel also appends the step's
@@ -852,7 +1017,143 @@ int32_t decode_attention_impl(odma_pool* pool, int32_t layer, const void* q, int
 
 }  // namespace
 
+namespace {
+
+// Where things lie in the workspace of a call behind a shared prefix of `len` keys.
+struct PrefixSpace {
+    int64_t rows = 0;           // query rows: one partial result of each per split
+    int64_t kv_bytes = 0;       // 8-bit pools: the prefix's keys and values as bf16
+    int32_t pad = 0;            // its rows per KV head
+    int64_t row_bytes = 0;      // of one row's partial result
+    uint64_t bytes(int32_t splits) const { return static_cast<uint64_t>(kv_bytes) + static_cast<uint64_t>(rows) * row_bytes * splits; }
+};
+
+PrefixSpace prefix_space(const odma_pool* pool, int32_t q_heads, int32_t n, int32_t len) {
+    PrefixSpace w;
+    w.rows = static_cast<int64_t>(n) * q_heads;
+    w.row_bytes = (static_cast<int64_t>(pool->head_dim) + 2) * 4;
+    w.pad = (len + kPrefixTile - 1) / kPrefixTile * kPrefixTile;
+    if (pool->dtype == ODMA_DTYPE_FP8_E4M3)
+        w.kv_bytes = 2ll * pool->kv_heads * w.pad * pool->head_dim * 2;
+    return w;
+}
+
+// Can the prefix's product run on the tensor cores?
+bool prefix_on_tensor(const odma_pool* pool) { return pool->has_maps && tc_supported(pool->head_dim, 1); }
+
+int32_t prefix_splits_of(const odma_pool* pool, int32_t q_heads, int32_t n, int32_t len) {
+    return len < 1 ? 0 : prefix_splits(n * (q_heads / pool->kv_heads), pool->kv_heads, len, pool->plan_ctas, prefix_on_tensor(pool));
+}
+
+bool prefix_shape_ok(const odma_pool* pool, int32_t q_heads, int32_t n, int32_t len) {
+    return n >= 1 && n <= pool->alloc.config().max_batch && len >= 0 && len <= pool->alloc.T() && q_heads >= pool->kv_heads &&
+           q_heads % pool->kv_heads == 0 && q_heads / pool->kv_heads <= pool->alloc.config().max_group &&
+           generic_supported(pool->head_dim) &&
+           (pool->dtype != ODMA_DTYPE_FP8_E4M3 || umma_supported(pool->head_dim, q_heads / pool->kv_heads, true));
+}
+
+}  // namespace
+
 extern "C" {
+
+uint64_t odma_prefix_workspace_bytes(const odma_pool* pool, int32_t q_heads, int32_t n, int32_t prefix_len) {
+    if (!pool || !prefix_shape_ok(pool, q_heads, n, prefix_len)) return 0;
+    const uint64_t b = prefix_space(pool, q_heads, n, prefix_len).bytes(prefix_splits_of(pool, q_heads, n, prefix_len));
+    return std::max<uint64_t>((b + 255) / 256 * 256, 256);
+}
+
+int32_t odma_decode_attention_prefix(odma_pool* pool, int32_t layer, const void* q, int32_t q_heads, uint64_t prefix_req,
+                                     int32_t prefix_len, const odma_tables* tables, void* workspace,
+                                     uint64_t workspace_bytes, void* out, float* lse, void* stream) {
+    int32_t rc = check_decode_args(pool, layer, q, q_heads, tables, out);
+    if (rc != ODMA_OK) return rc;
+    if (!prefix_shape_ok(pool, q_heads, tables->n, prefix_len)) return ODMA_ERR_INVALID;
+    const Request* pr = pool->alloc.find(prefix_req);
+    if (!pr) return ODMA_ERR_UNKNOWN_REQ;
+    if (prefix_len > pr->len) return ODMA_ERR_OVERFLOW;
+    if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return ODMA_ERR_INVALID;
+    const int32_t D = pool->head_dim, n = tables->n;
+    // as many splits of the prefix as are worth while, and as fit
+    const PrefixSpace w = prefix_space(pool, q_heads, n, prefix_len);
+    int32_t splits = prefix_splits_of(pool, q_heads, n, prefix_len);
+    if (splits > 0) {
+        if (!workspace || workspace_bytes < w.bytes(1)) return ODMA_ERR_INVALID;
+        splits = static_cast<int32_t>(std::min<int64_t>(splits, static_cast<int64_t>((workspace_bytes - w.kv_bytes) / (w.rows * w.row_bytes))));
+    }
+    cudaStream_t s = as_stream(stream);
+    DecodeParams p;
+    fill_decode_params(pool, layer, q, q_heads, tables, out, lse, &p);
+    p.counters = nullptr;
+    p.partial_only = 1;
+
+    pool->decode_was_last = false;               // other kernels of this call lie between decode launches
+    pool->last_fused_tensor = false;
+    const bool fp32 = pool->dtype == ODMA_DTYPE_F32;
+    PrefixParams pp{};
+    if (splits > 0) {
+        const int64_t row0 = pr->base * pool->kv_heads, k_row0 = static_cast<int64_t>(layer) * 2 * pool->rows_per_array + row0;
+        const uint8_t* k = static_cast<const uint8_t*>(pool->dev_base) + k_row0 * D * pool->elem_bytes;
+        const uint8_t* v = k + pool->rows_per_array * D * pool->elem_bytes;
+        pp.k = k;
+        pp.v = v;
+        pp.head_rows = pr->cap;
+        pp.q = q;
+        pp.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + w.kv_bytes);
+        pp.part_ml = pp.part_o + static_cast<int64_t>(splits) * w.rows * D;
+        pp.len = prefix_len;
+        pp.n = n;
+        pp.q_heads = q_heads;
+        pp.kv_heads = pool->kv_heads;
+        pp.group = p.group;
+        pp.head_dim = D;
+        pp.splits = splits;
+        pp.scale_log2 = p.scale_log2 * p.k_scale;
+        pp.status = pool->d_status;
+        pp.wait_limit_ns = p.wait_limit_ns;
+        pp.k_row0 = static_cast<int32_t>(k_row0);
+        pp.v_row0 = static_cast<int32_t>(k_row0 + pool->rows_per_array);
+        ProfScope ps(pool, ODMA_K_DECODE, s);
+        if (pool->dtype == ODMA_DTYPE_FP8_E4M3) {
+            if (launch_dequant_prefix(k, v, pr->cap, prefix_len, w.pad, pool->kv_heads, D, workspace, s) != cudaSuccess)
+                return ODMA_ERR_CUDA;
+            pp.k = workspace;
+            pp.v = static_cast<uint8_t*>(workspace) + w.kv_bytes / 2;
+            pp.head_rows = w.pad;
+        }
+        if (launch_prefix(pp, fp32, s) != cudaSuccess) return ODMA_ERR_CUDA;
+    }
+    {
+        ProfScope ps(pool, ODMA_K_DECODE, s);
+        cudaError_t e;
+        if (uses_tc(pool, q_heads)) {
+            if (p.stages < 2) return ODMA_ERR_INVALID;
+            e = launch_tensor_decode(pool, pool->maps, p, kModeSlab, tables, s, nullptr, uses_umma(pool, p.group, false));
+        } else {
+            e = launch_decode_generic(p, pool->dtype, tables->n_ctas, s);
+        }
+        if (e != cudaSuccess) return ODMA_ERR_CUDA;
+    }
+    MergePrefixParams m;
+    m.items = p.items;
+    m.combine = p.combine;
+    m.len = p.len;
+    m.own_o = p.part_o;
+    m.own_ml = p.part_ml;
+    m.part_o = pp.part_o;
+    m.part_ml = pp.part_ml;
+    m.out = out;
+    m.lse = lse;
+    m.n = n;
+    m.n_items = tables->n_items;
+    m.splits = splits;
+    m.q_heads = q_heads;
+    m.kv_heads = pool->kv_heads;
+    m.group = p.group;
+    m.head_dim = D;
+    m.v_scale = p.v_scale;
+    ProfScope ps(pool, ODMA_K_COMBINE, s);
+    return launch_merge_prefix(m, fp32, s) == cudaSuccess ? ODMA_OK : ODMA_ERR_CUDA;
+}
 
 int32_t odma_decode_attention(odma_pool* pool, int32_t layer, const void* q, int32_t q_heads,
                               const odma_tables* tables, void* out, float* lse, void* stream) {
@@ -1012,7 +1313,8 @@ int32_t odma_check_status(odma_pool* pool, void* stream) {
             cudaMemset(pool->d_counters, 0, static_cast<size_t>(pool->slots_max) * 8) != cudaSuccess)
             return ODMA_ERR_CUDA;
     }
-    return (word & kStatusTimeout) ? ODMA_ERR_TIMEOUT : ODMA_OK;
+    if (word & kStatusTimeout) return ODMA_ERR_TIMEOUT;
+    return (word & kStatusOverflow) ? ODMA_ERR_OVERFLOW : ODMA_OK;
 }
 
 int32_t odma_read_probe(odma_pool* pool, int32_t layer, int32_t q_heads, const odma_tables* tables,
@@ -1031,7 +1333,8 @@ int32_t odma_read_probe(odma_pool* pool, int32_t layer, int32_t q_heads, const o
     pool->decode_was_last = false;
     pool->last_fused_tensor = false;
     ProfScope ps(pool, ODMA_K_PROBE, as_stream(stream));
-    return launch_decode_tc(pool->maps, p, kModeProbe, tables->n_ctas, as_stream(stream)) == cudaSuccess
+    return launch_decode_tc(pool->maps, p, kModeProbe, tables->n_ctas, as_stream(stream), nullptr,
+                            !built_on_device(tables)) == cudaSuccess
                ? ODMA_OK
                : ODMA_ERR_CUDA;
 }

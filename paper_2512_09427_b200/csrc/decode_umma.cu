@@ -729,7 +729,7 @@ decode_umma_kernel(const __grid_constant__ TensorMaps tm, const DecodeParams p,
                     *reinterpret_cast<uint32_t*>(dst + 8 * i) = pack_bf16(x[2 * i] * inv, x[2 * i + 1] * inv);
                 if ((lane & 3) == 0 && lse_l) lse_l[row] = (M + fast_log2(Lsum)) * 0.6931471805599453f;
             };
-            if (im.direct) {
+            if (im.direct && !p.partial_only) {
 #pragma unroll
                 for (int rs = 0; rs < NT; ++rs) write_out(im.req, im.head, rs, m_ref[rs], l_acc[rs], oo[rs]);
                 return;
@@ -1101,7 +1101,7 @@ int umma_stages() {
 
 template <int D, int NT, int MODE, bool F8, bool DEFER>
 cudaError_t launch_umma_inst(const TensorMaps& maps, DecodeParams p, int n_ctas, cudaStream_t stream,
-                             const InlineLens& lens, const SpanParams& sp) {
+                             const InlineLens& lens, const SpanParams& sp, bool overlap) {
     using Cfg = UmmaConfig<D, NT, F8>;
     static bool configured[kMaxDevices] = {false};     // the opt-in to large shared memory is per device
     auto kern = decode_umma_kernel<D, NT, MODE, F8, DEFER>;
@@ -1126,18 +1126,18 @@ cudaError_t launch_umma_inst(const TensorMaps& maps, DecodeParams p, int n_ctas,
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // see griddepcontrol in the kernel
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = overlap ? 1 : 0;
     return cudaLaunchKernelEx(&cfg, kern, maps, p, lens, sp);
 }
 
 template <int D, int NT>
 cudaError_t launch_umma_mode(const TensorMaps& maps, const DecodeParams& p, int mode, int n_ctas, cudaStream_t s,
-                             const InlineLens& lens, const SpanParams& sp, bool defer) {
+                             const InlineLens& lens, const SpanParams& sp, bool defer, bool overlap) {
     switch (mode) {
         case kModeSlab:
-            return defer ? launch_umma_inst<D, NT, kModeSlab, false, true>(maps, p, n_ctas, s, lens, sp)
-                         : launch_umma_inst<D, NT, kModeSlab, false, false>(maps, p, n_ctas, s, lens, sp);
-        case kModePaged: return launch_umma_inst<D, NT, kModePaged, false, false>(maps, p, n_ctas, s, lens, sp);
+            return defer ? launch_umma_inst<D, NT, kModeSlab, false, true>(maps, p, n_ctas, s, lens, sp, overlap)
+                         : launch_umma_inst<D, NT, kModeSlab, false, false>(maps, p, n_ctas, s, lens, sp, overlap);
+        case kModePaged: return launch_umma_inst<D, NT, kModePaged, false, false>(maps, p, n_ctas, s, lens, sp, overlap);
     }
     return cudaErrorInvalidValue;
 }
@@ -1150,7 +1150,8 @@ bool umma_supported(int32_t head_dim, int32_t group, bool kv_fp8) {
 }
 
 cudaError_t launch_decode_umma(const TensorMaps& maps, const DecodeParams& p, int mode, int n_ctas,
-                               cudaStream_t stream, const InlineLens* lens_in, const SpanParams* span_in, bool defer) {
+                               cudaStream_t stream, const InlineLens* lens_in, const SpanParams* span_in, bool defer,
+                               bool overlap) {
     static const InlineLens no_lens{};                 // n = 0: lengths as planned
     static const SpanParams no_span{};                 // never read by a one-layer launch
     const InlineLens& lens = lens_in ? *lens_in : no_lens;
@@ -1158,15 +1159,15 @@ cudaError_t launch_decode_umma(const TensorMaps& maps, const DecodeParams& p, in
     const SpanParams& sp = span_in ? *span_in : no_span;
     if (p.kv_fp8) {
         if (!umma_supported(p.head_dim, p.group, true) || mode != kModeSlab) return cudaErrorInvalidValue;
-        return launch_umma_inst<128, 1, kModeSlab, true, false>(maps, p, n_ctas, stream, lens, sp);
+        return launch_umma_inst<128, 1, kModeSlab, true, false>(maps, p, n_ctas, stream, lens, sp, overlap);
     }
     const bool two = p.group > 8;
     if (p.head_dim == 128)
-        return two ? launch_umma_mode<128, 2>(maps, p, mode, n_ctas, stream, lens, sp, defer)
-                   : launch_umma_mode<128, 1>(maps, p, mode, n_ctas, stream, lens, sp, defer);
+        return two ? launch_umma_mode<128, 2>(maps, p, mode, n_ctas, stream, lens, sp, defer, overlap)
+                   : launch_umma_mode<128, 1>(maps, p, mode, n_ctas, stream, lens, sp, defer, overlap);
     if (p.head_dim == 64)
-        return two ? launch_umma_mode<64, 2>(maps, p, mode, n_ctas, stream, lens, sp, defer)
-                   : launch_umma_mode<64, 1>(maps, p, mode, n_ctas, stream, lens, sp, defer);
+        return two ? launch_umma_mode<64, 2>(maps, p, mode, n_ctas, stream, lens, sp, defer, overlap)
+                   : launch_umma_mode<64, 1>(maps, p, mode, n_ctas, stream, lens, sp, defer, overlap);
     return cudaErrorInvalidValue;
 }
 

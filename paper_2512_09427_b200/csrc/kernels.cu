@@ -350,7 +350,7 @@ decode_tc_kernel(const __grid_constant__ TensorMaps tm, const DecodeParams p,
                 dsc[0] = req;
                 dsc[1] = head;
                 dsc[2] = ntok;
-                dsc[3] = b.x & 1;                        // direct
+                dsc[3] = p.partial_only ? 0 : b.x & 1;   // direct
                 dsc[4] = b.y;                            // slot
                 dsc[5] = b.w;                            // combine record
                 dsc[6] = 1;                              // a real item
@@ -897,7 +897,8 @@ decode_generic_kernel(const DecodeParams p) {
     const int4 rec = __ldg(p.cta + 3 * cta);
     for (int it = rec.x; it < rec.y; ++it) {
         const int4 a = p.items[2 * it], b = p.items[2 * it + 1];
-        const int req = a.x, head = a.y, tok0 = a.z, ntok = a.w, direct = b.x & 1, slot = b.y;
+        const int req = a.x, head = a.y, tok0 = a.z, ntok = a.w, slot = b.y;
+        const int direct = p.partial_only ? 0 : b.x & 1;
         const int64_t row0 = static_cast<int64_t>(p.base[req]) * p.kv_heads +
                              static_cast<int64_t>(head) * p.cap[req] + tok0;
         const T* K = pool + (static_cast<int64_t>(p.layer) * 2 * p.rows_per_array + row0) * D;
@@ -1028,6 +1029,7 @@ combine_kernel(const int4* __restrict__ combine, const float* __restrict__ part_
                const float* __restrict__ part_ml, T* __restrict__ out, float* __restrict__ lse,
                int group, int D, int q_heads) {
     const int4 rec = combine[blockIdx.x];
+    if (rec.w <= 0) return;                            // a device-built table's unused record
     combine_stream(part_o, part_ml, rec.z, rec.w, rec.x, rec.y, group, D, q_heads, out, lse,
                    static_cast<int>(threadIdx.x), static_cast<int>(blockDim.x));
 }
@@ -1061,6 +1063,8 @@ __global__ void __launch_bounds__(256) append_kv_kernel(const AppendParams p) {
         }
         const int n_new = p.cu_new[req + 1] - p.cu_new[req];
         const int pos = p.len[req] - n_new + (tok - p.cu_new[req]);
+        // device-built tables: the row belongs to no request, or to a refused one
+        if (pos < 0 || tok >= p.cu_new[req] + n_new) continue;
         const int64_t row = static_cast<int64_t>(p.base[req]) * p.kv_heads +
                             static_cast<int64_t>(head) * p.cap[req] + pos;
         const int64_t array = static_cast<int64_t>(p.layer) * 2 + kv;
@@ -1129,7 +1133,7 @@ constexpr int kSmemCtaReserve = 1024;     // what the system keeps per resident 
 
 template <int D, int NT, int MODE>
 cudaError_t launch_tc_inst(const TensorMaps& maps, const DecodeParams& p, int n_ctas, cudaStream_t stream,
-                           const InlineLens& lens) {
+                           const InlineLens& lens, bool overlap) {
     using Cfg = TcConfig<D, NT>;
     static bool configured[64] = {false};          // the opt-in to large shared memory is per device
     auto kern = decode_tc_kernel<D, NT, MODE>;
@@ -1155,17 +1159,17 @@ cudaError_t launch_tc_inst(const TensorMaps& maps, const DecodeParams& p, int n_
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;   // see griddepcontrol in the kernel
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = overlap ? 1 : 0;
     return cudaLaunchKernelEx(&cfg, kern, maps, p, lens);
 }
 
 template <int D, int NT>
 cudaError_t launch_tc_mode(const TensorMaps& maps, const DecodeParams& p, int mode, int n_ctas, cudaStream_t s,
-                           const InlineLens& lens) {
+                           const InlineLens& lens, bool overlap) {
     switch (mode) {
-        case kModeSlab: return launch_tc_inst<D, NT, kModeSlab>(maps, p, n_ctas, s, lens);
-        case kModePaged: return launch_tc_inst<D, NT, kModePaged>(maps, p, n_ctas, s, lens);
-        case kModeProbe: return launch_tc_inst<D, NT, kModeProbe>(maps, p, n_ctas, s, lens);
+        case kModeSlab: return launch_tc_inst<D, NT, kModeSlab>(maps, p, n_ctas, s, lens, overlap);
+        case kModePaged: return launch_tc_inst<D, NT, kModePaged>(maps, p, n_ctas, s, lens, overlap);
+        case kModeProbe: return launch_tc_inst<D, NT, kModeProbe>(maps, p, n_ctas, s, lens, overlap);
     }
     return cudaErrorInvalidValue;
 }
@@ -1219,16 +1223,16 @@ void tc_shape(int32_t head_dim, int32_t group, int32_t* stages, int32_t* q_slots
 }
 
 cudaError_t launch_decode_tc(const TensorMaps& maps, const DecodeParams& p, int mode, int n_ctas,
-                             cudaStream_t stream, const InlineLens* lens_in) {
+                             cudaStream_t stream, const InlineLens* lens_in, bool overlap) {
     static const InlineLens no_lens{};                 // n = 0: lengths as planned
     const InlineLens& lens = lens_in ? *lens_in : no_lens;
     const bool two = p.group > 8;
     if (p.head_dim == 128)
-        return two ? launch_tc_mode<128, 2>(maps, p, mode, n_ctas, stream, lens)
-                   : launch_tc_mode<128, 1>(maps, p, mode, n_ctas, stream, lens);
+        return two ? launch_tc_mode<128, 2>(maps, p, mode, n_ctas, stream, lens, overlap)
+                   : launch_tc_mode<128, 1>(maps, p, mode, n_ctas, stream, lens, overlap);
     if (p.head_dim == 64)
-        return two ? launch_tc_mode<64, 2>(maps, p, mode, n_ctas, stream, lens)
-                   : launch_tc_mode<64, 1>(maps, p, mode, n_ctas, stream, lens);
+        return two ? launch_tc_mode<64, 2>(maps, p, mode, n_ctas, stream, lens, overlap)
+                   : launch_tc_mode<64, 1>(maps, p, mode, n_ctas, stream, lens, overlap);
     return cudaErrorInvalidValue;
 }
 

@@ -10,6 +10,7 @@ namespace odma {
 
 // Status word bits written by kernels.
 constexpr uint32_t kStatusTimeout = 1u;
+constexpr uint32_t kStatusOverflow = 2u;    // a request of a device-built table was refused
 
 struct DecodeParams {
     // per-step tables (device)
@@ -52,6 +53,7 @@ struct DecodeParams {
     // (same plan, the pipeline never drains); layer li of the launch uses K/V arrays of layer + li and
     // the buffers below advanced by li strides.
     int32_t n_layers;           // 1 = the usual launch; more: see SpanParams
+    int32_t partial_only;       // every item leaves a partial result, whole streams too (counters is nullptr then)
     int32_t stages;             // pipeline depth of the tensor-core kernel (2..8)
     int32_t q_slots;            // depth of its query / item-descriptor ring (4..8)
 };
@@ -88,8 +90,10 @@ bool tc_supported(int32_t head_dim, int32_t group);
 // Pipeline stages and query-ring slots that fit into one SM's shared memory (one CTA per SM;
 // both 0 when nothing fits).
 void tc_shape(int32_t head_dim, int32_t group, int32_t* stages, int32_t* q_slots);
+// `overlap`: launched with programmatic stream serialization (the kernel reads its plan before it waits for
+// the kernel ahead); false where that kernel may be the one that writes the plan.
 cudaError_t launch_decode_tc(const TensorMaps& maps, const DecodeParams& p, int mode, int n_ctas,
-                             cudaStream_t stream, const InlineLens* lens = nullptr);
+                             cudaStream_t stream, const InlineLens* lens = nullptr, bool overlap = true);
 // The same decode step on the tcgen05 tensor cores (decode_umma.cu): slab and paged modes;
 // `stages` and `q_slots` of the parameter block are ignored (the kernel sizes its own rings).
 // An 8-bit (E4M3) pool: head_dim 128, group <= 8, slab mode.  `defer` (16-bit slabs, slab mode)
@@ -97,7 +101,7 @@ cudaError_t launch_decode_tc(const TensorMaps& maps, const DecodeParams& p, int 
 bool umma_supported(int32_t head_dim, int32_t group, bool kv_fp8);
 cudaError_t launch_decode_umma(const TensorMaps& maps, const DecodeParams& p, int mode, int n_ctas,
                                cudaStream_t stream, const InlineLens* lens = nullptr, const SpanParams* span = nullptr,
-                               bool defer = false);
+                               bool defer = false, bool overlap = true);
 cudaError_t launch_decode_generic(const DecodeParams& p, int dtype, int n_ctas, cudaStream_t stream);
 bool generic_supported(int32_t head_dim);
 
@@ -121,6 +125,86 @@ struct AppendParams {
     float k_inv, v_inv;         // fp32 and rounded to the nearest code (row_vecs counts the stored row)
 };
 cudaError_t launch_append(const AppendParams& p, cudaStream_t stream);
+
+// Tables built on the GPU (tables.cu): limits of one call, and its arguments.
+constexpr int kMaxDeviceBatch = 4096;
+constexpr int kMaxDeviceCtas = 1024;
+struct DeviceTablesParams {
+    const int32_t* slabs;       // [n][2] base, capacity
+    const int32_t* len;         // [n] tokens before the step
+    const int32_t* n_new;       // [n] tokens of the step; nullptr: one each
+    int32_t* len_next;          // [n] tokens after the step, may be `len`; or nullptr
+    int32_t* slots;             // [n_new_total] row of KV head 0 inside one K (or V) array, or nullptr
+    int32_t* positions;         // [n_new_total] position in the slab, or nullptr
+    int32_t* table;
+    uint32_t* status;
+    int64_t tokens;             // capacity of the pool
+    int32_t n, kv_heads, n_ctas, n_new_total;
+    int32_t n_items, n_combine; // room for items and combine records
+    int32_t off_base, off_cap, off_len, off_cu_new, off_cta, off_items, off_combine;
+};
+cudaError_t launch_build_tables(const DeviceTablesParams& p, cudaStream_t stream);
+
+// Norm, rotation and append in one pass (qkv.cu).
+constexpr int kMaxRotPairs = 128;
+constexpr int kMaxAxes = 4;
+struct QkvParams {
+    const int32_t* base;        // the step's table
+    const int32_t* cap;
+    const int32_t* len;
+    const int32_t* cu_new;
+    void* pool;
+    const void* q;
+    const void* k_new;
+    const void* v_new;
+    void* q_out;
+    const void* q_norm;         // [head_dim] or nullptr
+    const void* k_norm;
+    const float* inv_freq;      // [rot_pairs]
+    const int32_t* positions;   // [n_axes] rows of pos_stride, or nullptr: the token's slab position
+    int64_t q_stride, k_stride, v_stride, pos_stride;   // elements between tokens; positions between axes
+    int64_t rows_per_array;
+    int32_t layer, n, q_heads, kv_heads, head_dim, n_new_total, one_new_each, quantize;
+    int32_t rot_pairs, interleaved, n_axes;
+    int32_t section_end[kMaxAxes];
+    float eps, k_inv, v_inv;
+};
+cudaError_t launch_append_qkv(const QkvParams& p, bool fp32, cudaStream_t stream);
+
+// Attention behind a shared prefix (prefix.cu).
+constexpr int kPrefixTile = 128;      // keys per tile; splits are whole tiles
+constexpr int kMaxPrefixSplits = 128;
+struct PrefixParams {
+    const void* k;              // the prefix's first key (value) row of KV head 0
+    const void* v;
+    int64_t head_rows;          // rows between KV heads
+    const void* q;              // [n, q_heads, head_dim]
+    float* part_o;              // [splits][n * q_heads][head_dim]
+    float* part_ml;             // [splits][n * q_heads][2]
+    int32_t len, n, q_heads, kv_heads, group, head_dim, splits;
+    float scale_log2;
+    uint32_t* status;
+    int64_t wait_limit_ns;
+    int32_t k_row0, v_row0;     // rows of k and v in the tensor maps' array
+};
+struct MergePrefixParams {
+    const int4* items;
+    const int4* combine;
+    const int32_t* len;
+    const float* own_o;         // [slots][group][head_dim]
+    const float* own_ml;
+    const float* part_o;
+    const float* part_ml;
+    void* out;
+    float* lse;
+    int32_t n, n_items, splits, q_heads, kv_heads, group, head_dim;
+    float v_scale;              // of the prefix's partial results
+};
+int32_t prefix_splits(int32_t rows, int32_t kv_heads, int32_t len, int32_t sms, bool tensor);
+cudaError_t launch_prefix(const PrefixParams& p, bool fp32, cudaStream_t stream);
+cudaError_t launch_dequant_prefix(const void* k, const void* v, int64_t head_rows, int32_t len, int32_t pad,
+                                  int32_t kv_heads, int32_t head_dim, void* out, cudaStream_t stream);
+cudaError_t launch_merge_prefix(const MergePrefixParams& p, bool fp32, cudaStream_t stream);
 
 struct MigrateParams {
     void* pool;

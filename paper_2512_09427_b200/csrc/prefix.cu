@@ -1,0 +1,288 @@
+// Decode attention of a batch whose requests share a prefix (odma_decode_attention_prefix).
+//
+// For query row r = (request, query head) of KV head h, prefix keys K_P (one slab, shared) and the
+// request's own keys K_i:
+//     out_r = softmax([q_r . K_P^T, q_r . K_i^T] / sqrt(D)) [V_P; V_i]
+// The prefix part is computed for all n * g rows of a KV head at once, so the prefix is read once (per
+// tile of rows) and not once per request: per split s of its keys a row leaves (m, l, o) = (running
+// maximum in log2 units, sum of 2^(x - m), unnormalised output) in the caller's workspace.  The
+// requests' own parts come from the decode kernels, every piece left as a partial result.
+// merge_prefix_kernel folds both with the log-sum-exp rule and rounds once.
+//
+//  prefix_generic_kernel   plain ALUs, fp32 arithmetic: fp32 slabs, head_dim 32
+//  dequant_prefix_kernel   8-bit slabs: the prefix's codes as bf16 (exact: a code has 4 significant
+//                          bits); the scales stay outside, in the score factor and in the merge
+//  merge_prefix_kernel     own pieces and prefix splits to out and lse
+#include <algorithm>
+
+#include "device_utils.cuh"
+#include "odma.h"
+
+namespace odma {
+namespace {
+
+using namespace dev;
+
+constexpr int kRows = 8;            // query rows a block of the generic kernel carries
+constexpr int kWarps = 4;
+
+__device__ __forceinline__ void unpack16(const uint4& v, float (&x)[4], float) {
+    x[0] = __uint_as_float(v.x);
+    x[1] = __uint_as_float(v.y);
+    x[2] = __uint_as_float(v.z);
+    x[3] = __uint_as_float(v.w);
+}
+__device__ __forceinline__ void unpack16(const uint4& v, float (&x)[8], __nv_bfloat16) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = __uint_as_float(w[i] << 16);
+        x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ float as_float(float x) { return x; }
+__device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+// Keys [first, last) of split s: the prefix's tiles of 128 keys dealt evenly.
+__device__ __forceinline__ void split_range(const PrefixParams& p, int s, int& first, int& last) {
+    const int tiles = (p.len + kPrefixTile - 1) / kPrefixTile;
+    first = static_cast<int>(static_cast<int64_t>(tiles) * s / p.splits) * kPrefixTile;
+    last = min(p.len, static_cast<int>(static_cast<int64_t>(tiles) * (s + 1) / p.splits) * kPrefixTile);
+}
+
+template <typename T, int DPL>      // head_dim = 32 * DPL
+__global__ void __launch_bounds__(kWarps * 32) prefix_generic_kernel(const PrefixParams p) {
+    constexpr int D = 32 * DPL;
+    constexpr int VE = 16 / sizeof(T);
+    __shared__ float q_s[kRows][D];
+    __shared__ float p_s[kWarps][kRows][32];
+    __shared__ float mrg_o[kWarps][kRows][D];
+    __shared__ float mrg_ml[kWarps][kRows][2];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int head = blockIdx.y, rows = p.n * p.group, r0 = blockIdx.x * kRows;
+    int first, last;
+    split_range(p, blockIdx.z, first, last);
+    const T* K = static_cast<const T*>(p.k) + static_cast<int64_t>(head) * p.head_rows * D;
+    const T* V = static_cast<const T*>(p.v) + static_cast<int64_t>(head) * p.head_rows * D;
+    auto out_row = [&](int r) { return static_cast<int64_t>(r / p.group) * p.q_heads + head * p.group + r % p.group; };
+    for (int i = tid; i < kRows * D; i += kWarps * 32) {
+        const int r = r0 + i / D;
+        q_s[i / D][i % D] = r < rows ? as_float(static_cast<const T*>(p.q)[out_row(r) * D + i % D]) : 0.f;
+    }
+    __syncthreads();
+    float m[kRows], l[kRows], o[kRows][DPL];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+        m[r] = -INFINITY;
+        l[r] = 0.f;
+#pragma unroll
+        for (int c = 0; c < DPL; ++c) o[r][c] = 0.f;
+    }
+    for (int j0 = first + warp * 32; j0 < last; j0 += kWarps * 32) {
+        const bool valid = j0 + lane < last;
+        float s[kRows];
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) s[r] = 0.f;
+        if (valid) {
+            const uint4* kp = reinterpret_cast<const uint4*>(K + static_cast<int64_t>(j0 + lane) * D);
+#pragma unroll 4
+            for (int v = 0; v < D / VE; ++v) {
+                float x[VE];
+                unpack16(__ldg(kp + v), x, T());
+#pragma unroll
+                for (int e = 0; e < VE; ++e)
+#pragma unroll
+                    for (int r = 0; r < kRows; ++r) s[r] = fmaf(q_s[r][v * VE + e], x[e], s[r]);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < kRows; ++r) {
+            const float x = valid ? s[r] * p.scale_log2 : -INFINITY;
+            float mx = x;
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, off));
+            const float m_new = fmaxf(m[r], mx);
+            // a maximum of -inf (every score so far is) contributes nothing and must not make NaN of it
+            const float pr = m_new == -INFINITY ? 0.f : exp2f(x - m_new);
+            const float corr = m_new == -INFINITY ? 1.f : exp2f(m[r] - m_new);
+            float ps = pr;
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) ps += __shfl_xor_sync(0xFFFFFFFFu, ps, off);
+            l[r] = fmaf(l[r], corr, ps);
+            m[r] = m_new;
+#pragma unroll
+            for (int c = 0; c < DPL; ++c) o[r][c] *= corr;
+            p_s[warp][r][lane] = pr;
+        }
+        __syncwarp();
+        const int cnt = min(32, last - j0);
+        for (int jj = 0; jj < cnt; ++jj) {
+            float v[DPL];
+#pragma unroll
+            for (int c = 0; c < DPL; ++c) v[c] = as_float(V[static_cast<int64_t>(j0 + jj) * D + lane + 32 * c]);
+#pragma unroll
+            for (int r = 0; r < kRows; ++r) {
+                const float pr = p_s[warp][r][jj];
+#pragma unroll
+                for (int c = 0; c < DPL; ++c) o[r][c] = fmaf(pr, v[c], o[r][c]);
+            }
+        }
+        __syncwarp();
+    }
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+#pragma unroll
+        for (int c = 0; c < DPL; ++c) mrg_o[warp][r][lane + 32 * c] = o[r][c];
+        if (lane == 0) {
+            mrg_ml[warp][r][0] = m[r];
+            mrg_ml[warp][r][1] = l[r];
+        }
+    }
+    __syncthreads();
+    for (int i = tid; i < kRows * D; i += kWarps * 32) {
+        const int r = i / D, d = i % D;
+        if (r0 + r >= rows) break;
+        float M = -INFINITY, L = 0.f, O = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) M = fmaxf(M, mrg_ml[w][r][0]);
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            const float e = mrg_ml[w][r][0] == -INFINITY ? 0.f : exp2f(mrg_ml[w][r][0] - M);
+            L = fmaf(mrg_ml[w][r][1], e, L);
+            O = fmaf(mrg_o[w][r][d], e, O);
+        }
+        const int64_t at = static_cast<int64_t>(blockIdx.z) * p.n * p.q_heads + out_row(r0 + r);
+        p.part_o[at * D + d] = O;
+        if (d == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * at) = make_float2(M, L);
+    }
+}
+
+// Codes [kv_heads][len][D] of K and V (rows of a head head_rows apart) to bf16 [2][kv_heads][pad][D].
+__global__ void __launch_bounds__(256) dequant_prefix_kernel(const uint8_t* k, const uint8_t* v, int64_t head_rows, int len,
+                                                             int pad, int kv_heads, int D, __nv_bfloat16* out) {
+    const int head = blockIdx.y % kv_heads;
+    const uint8_t* src = (blockIdx.y < kv_heads ? k : v) + head * head_rows * D;
+    __nv_bfloat16* dst = out + static_cast<int64_t>(blockIdx.y) * pad * D;
+    const int64_t vecs = static_cast<int64_t>(len) * D / 16;
+    for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < vecs; i += static_cast<int64_t>(gridDim.x) * blockDim.x) {
+        const uint4 c = __ldg(reinterpret_cast<const uint4*>(src) + i);
+        const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+        uint32_t o[8];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float2 lo = unpack_e4m3(w[j]), hi = unpack_e4m3(w[j] >> 16);
+            o[2 * j] = pack_bf16(lo.x, lo.y);
+            o[2 * j + 1] = pack_bf16(hi.x, hi.y);
+        }
+        uint4* to = reinterpret_cast<uint4*>(dst) + 2 * i;
+        to[0] = make_uint4(o[0], o[1], o[2], o[3]);
+        to[1] = make_uint4(o[4], o[5], o[6], o[7]);
+    }
+}
+
+// Blocks [0, n_items): the stream that begins with this item.  Blocks behind them: the requests, for
+// those without a token of their own.
+template <typename T>
+__global__ void __launch_bounds__(128) merge_prefix_kernel(const MergePrefixParams p) {
+    int req, head, heads = 1, slot0 = 0, pieces = 0;
+    if (static_cast<int>(blockIdx.x) < p.n_items) {
+        const int4 a = __ldg(p.items + 2 * blockIdx.x), b = __ldg(p.items + 2 * blockIdx.x + 1);
+        if (a.x < 0 || a.z != 0) return;               // unused, or not a stream's first piece
+        req = a.x;
+        head = a.y;
+        slot0 = b.y;
+        pieces = b.w < 0 ? 1 : __ldg(p.combine + b.w).w;
+    } else {
+        req = static_cast<int>(blockIdx.x) - p.n_items;
+        if (__ldg(p.len + req) > 0) return;
+        head = 0;
+        heads = p.kv_heads;
+    }
+    const int D = p.head_dim, per_row = D >> 2;
+    const int64_t split_rows = static_cast<int64_t>(p.n) * p.q_heads;
+    for (int idx = threadIdx.x; idx < heads * p.group * per_row; idx += blockDim.x) {
+        const int g = idx / per_row, d0 = (idx - g * per_row) * 4;
+        const int64_t row = static_cast<int64_t>(req) * p.q_heads + head * p.group + g;
+        float M = -INFINITY, L = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+        for (int s = 0; s < pieces; ++s) {
+            const int64_t at = static_cast<int64_t>(slot0 + s) * p.group + g;
+            const float2 ml = __ldcg(reinterpret_cast<const float2*>(p.own_ml + 2 * at));
+            lse_fold(M, L, acc, ml.x, ml.y, ldcg4(p.own_o + at * D + d0));
+        }
+#pragma unroll 4
+        for (int s = 0; s < p.splits; ++s) {
+            const int64_t at = s * split_rows + row;
+            const float2 ml = __ldcg(reinterpret_cast<const float2*>(p.part_ml + 2 * at));
+            float4 x = ldcg4(p.part_o + at * D + d0);
+            x.x *= p.v_scale;
+            x.y *= p.v_scale;
+            x.z *= p.v_scale;
+            x.w *= p.v_scale;
+            lse_fold(M, L, acc, ml.x, ml.y, x);
+        }
+        const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);      // no key at all: zeros
+        store4(static_cast<T*>(p.out) + row * D + d0, acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
+        if (d0 == 0 && p.lse) p.lse[row] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+    }
+}
+
+template <typename T>
+cudaError_t launch_generic_t(const PrefixParams& p, cudaStream_t s) {
+    const dim3 grid(static_cast<unsigned>((p.n * p.group + kRows - 1) / kRows), static_cast<unsigned>(p.kv_heads),
+                    static_cast<unsigned>(p.splits));
+    switch (p.head_dim) {
+        case 32: prefix_generic_kernel<T, 1><<<grid, kWarps * 32, 0, s>>>(p); break;
+        case 64: prefix_generic_kernel<T, 2><<<grid, kWarps * 32, 0, s>>>(p); break;
+        case 128: prefix_generic_kernel<T, 4><<<grid, kWarps * 32, 0, s>>>(p); break;
+        default: return cudaErrorInvalidValue;
+    }
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+int32_t prefix_splits(int32_t rows, int32_t kv_heads, int32_t len, int32_t sms, bool tensor) {
+    // Splits of the prefix's keys: enough blocks to fill the SMs, counted in waves, against what every
+    // split adds (a block's start-up and hand-over; a partial result to write and fold).
+    (void)tensor;
+    const int64_t tiles = (len + kPrefixTile - 1) / kPrefixTile;
+    const int64_t blocks = static_cast<int64_t>((rows + kRows - 1) / kRows) * kv_heads, room = 4ll * sms;
+    int32_t best = 1;
+    int64_t least = INT64_MAX;
+    for (int32_t s = 1; s <= std::min<int64_t>(tiles, kMaxPrefixSplits); ++s) {
+        const int64_t waves = (blocks * s + room - 1) / room;
+        const int64_t cost = waves * ((tiles + s - 1) / s * 4 + 2) + s / 4;
+        if (cost < least) {
+            least = cost;
+            best = s;
+        }
+    }
+    return best;
+}
+
+cudaError_t launch_prefix(const PrefixParams& p, bool fp32, cudaStream_t stream) {
+    if (p.splits < 1 || p.len < 1) return cudaSuccess;
+    return fp32 ? launch_generic_t<float>(p, stream) : launch_generic_t<__nv_bfloat16>(p, stream);
+}
+
+cudaError_t launch_dequant_prefix(const void* k, const void* v, int64_t head_rows, int32_t len, int32_t pad,
+                                  int32_t kv_heads, int32_t head_dim, void* out, cudaStream_t stream) {
+    const int64_t blocks = (static_cast<int64_t>(len) * head_dim / 16 + 255) / 256;
+    const dim3 grid(static_cast<unsigned>(std::min<int64_t>(blocks, 256)), static_cast<unsigned>(2 * kv_heads));
+    dequant_prefix_kernel<<<grid, 256, 0, stream>>>(static_cast<const uint8_t*>(k), static_cast<const uint8_t*>(v), head_rows, len,
+                                                    pad, kv_heads, head_dim, static_cast<__nv_bfloat16*>(out));
+    return cudaGetLastError();
+}
+
+cudaError_t launch_merge_prefix(const MergePrefixParams& p, bool fp32, cudaStream_t stream) {
+    const int grid = p.n_items + p.n;
+    if (fp32)
+        merge_prefix_kernel<float><<<grid, 128, 0, stream>>>(p);
+    else
+        merge_prefix_kernel<__nv_bfloat16><<<grid, 128, 0, stream>>>(p);
+    return cudaGetLastError();
+}
+
+}  // namespace odma

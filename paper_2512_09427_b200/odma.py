@@ -82,6 +82,21 @@ class SimResult(C.Structure):
         return {k: int(getattr(self, k)) for k, _ in self._fields_}
 
 
+class QkvPrep(C.Structure):
+    """odma_qkv_prep: what odma_append_qkv does to the heads.  Pointers as integers (0 = none); `section`: pairs per
+    position axis (one entry, or none: one axis); strides in elements (0 = packed)."""
+    _fields_ = [("q_norm", C.c_void_p), ("k_norm", C.c_void_p), ("inv_freq", C.c_void_p), ("positions", C.c_void_p),
+                ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("pos_stride", C.c_int64),
+                ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("n_axes", C.c_int32), ("section", C.c_int32 * 4),
+                ("eps", C.c_float)]
+
+    def __init__(self, rot_dim: int = 0, interleaved: bool = False, section: Sequence[int] = (), inv_freq: int = 0,
+                 positions: int = 0, q_norm: int = 0, k_norm: int = 0, eps: float = 1e-6, q_stride: int = 0,
+                 k_stride: int = 0, v_stride: int = 0, pos_stride: int = 0):
+        super().__init__(q_norm or None, k_norm or None, inv_freq or None, positions or None, q_stride, k_stride,
+                         v_stride, pos_stride, rot_dim, int(interleaved), max(1, len(section)), (C.c_int32 * 4)(*section), eps)
+
+
 SIM_STATIC, SIM_PAGED16, SIM_ODMA = 0, 1, 2
 
 _vp, _i32, _u64, _i64 = C.c_void_p, C.c_int32, C.c_uint64, C.c_int64
@@ -109,6 +124,11 @@ _SIGS = {
     "odma_plan_host": (_i32, [_vp, _u64p, _i32p, _i32, _i32p, _u64, C.POINTER(Tables)]),
     "odma_build_tables": (_i32, [_vp, _u64p, _i32p, _i32, _vp, _u64, _vp, C.POINTER(Tables)]),
     "odma_build_prefill_tables": (_i32, [_vp, _u64p, _i32p, _i32, _vp, _u64, _vp, C.POINTER(Tables)]),
+    "odma_slab_table": (_i32, [_vp, _u64p, _i32, _vp, _vp, _vp]),
+    "odma_build_tables_device": (_i32, [_vp, _vp, _vp, _vp, _i32, _i32, _vp, _u64, _vp, _vp, _vp, _vp, C.POINTER(Tables)]),
+    "odma_append_qkv": (_i32, [_vp, _i32, C.POINTER(Tables), _vp, _vp, _vp, _vp, _i32, C.POINTER(QkvPrep), _vp]),
+    "odma_prefix_workspace_bytes": (_u64, [_vp, _i32, _i32, _i32]),
+    "odma_decode_attention_prefix": (_i32, [_vp, _i32, _vp, _i32, _u64, _i32, C.POINTER(Tables), _vp, _u64, _vp, _vp, _vp]),
     "odma_append_kv": (_i32, [_vp, _i32, C.POINTER(Tables), _vp, _vp, _vp]),
     "odma_decode_attention": (_i32, [_vp, _i32, _vp, _i32, C.POINTER(Tables), _vp, _vp, _vp]),
     "odma_decode_step_host": (_i32, [_vp, _i32, _i32, _u64p, _i32, _vp, _vp, _vp, _vp, _vp]),
@@ -275,7 +295,38 @@ class Pool:
                                               table_bytes, stream or None, C.byref(t)), "odma_build_prefill_tables")
         return t
 
+    def slab_table(self, reqs: Sequence[int], d_slabs: int, d_len: int = 0, stream: int = 0) -> None:
+        """Slabs ([n][2]: base, capacity) and committed lengths of live requests to device memory."""
+        _check(_lib.odma_slab_table(self._h, _u64arr(reqs), len(reqs), d_slabs, d_len or None, stream or None),
+               "odma_slab_table")
+
+    def build_tables_device(self, d_slabs: int, d_len: int, n: int, n_new_total: int, d_table: int, table_bytes: int,
+                            d_n_new: int = 0, d_len_next: int = 0, d_slots: int = 0, d_positions: int = 0,
+                            stream: int = 0) -> Tables:
+        """The step's table, slot map and positions from lengths in device memory: one kernel, may be captured."""
+        t = Tables()
+        _check(_lib.odma_build_tables_device(self._h, d_slabs, d_len, d_n_new or None, n, n_new_total, d_table,
+                                             table_bytes, d_len_next or None, d_slots or None, d_positions or None,
+                                             stream or None, C.byref(t)), "odma_build_tables_device")
+        return t
+
     # -- kernels -----------------------------------------------------------------------------
+    def append_qkv(self, layer: int, tables: Tables, q: int, k_new: int, v_new: int, q_out: int, q_heads: int,
+                   prep: QkvPrep, stream: int = 0) -> None:
+        """Norm and rotation of the step's query and key heads, queries to q_out, keys and values to the slabs."""
+        _check(_lib.odma_append_qkv(self._h, layer, C.byref(tables), q, k_new, v_new, q_out, q_heads, C.byref(prep),
+                                    stream or None), "odma_append_qkv")
+
+    def prefix_workspace_bytes(self, q_heads: int, n: int, prefix_len: int) -> int:
+        return int(_lib.odma_prefix_workspace_bytes(self._h, q_heads, n, prefix_len))
+
+    def decode_attention_prefix(self, layer: int, q: int, q_heads: int, prefix_req: int, prefix_len: int, tables: Tables,
+                                workspace: int, workspace_bytes: int, out: int, lse: int = 0, stream: int = 0) -> None:
+        """Decode attention of a batch whose requests share the first prefix_len tokens of prefix_req's slab."""
+        _check(_lib.odma_decode_attention_prefix(self._h, layer, q, q_heads, prefix_req, prefix_len, C.byref(tables),
+                                                 workspace or None, workspace_bytes, out, lse or None, stream or None),
+               "odma_decode_attention_prefix")
+
     def append_kv(self, layer: int, tables: Tables, k_new: int, v_new: int, stream: int = 0) -> None:
         _check(_lib.odma_append_kv(self._h, layer, C.byref(tables), k_new, v_new, stream or None),
                "odma_append_kv")
