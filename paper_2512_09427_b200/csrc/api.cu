@@ -1038,11 +1038,12 @@ PrefixSpace prefix_space(const odma_pool* pool, int32_t q_heads, int32_t n, int3
     return w;
 }
 
-// Can the prefix's product run on the tensor cores?
-bool prefix_on_tensor(const odma_pool* pool) { return pool->has_maps && tc_supported(pool->head_dim, 1); }
+// Does the prefix's product run on the tensor cores?  (Asked of bookkeeping-only pools too.)
+bool prefix_on_tensor(const odma_pool* pool) { return pool->dtype != ODMA_DTYPE_F32 && tc_supported(pool->head_dim, 1); }
 
 int32_t prefix_splits_of(const odma_pool* pool, int32_t q_heads, int32_t n, int32_t len) {
-    return len < 1 ? 0 : prefix_splits(n * (q_heads / pool->kv_heads), pool->kv_heads, len, pool->plan_ctas, prefix_on_tensor(pool));
+    return len < 1 ? 0 : prefix_splits(n * (q_heads / pool->kv_heads), n * q_heads, pool->kv_heads, len, pool->plan_ctas,
+                                       prefix_on_tensor(pool));
 }
 
 bool prefix_shape_ok(const odma_pool* pool, int32_t q_heads, int32_t n, int32_t len) {
@@ -1080,6 +1081,8 @@ int32_t odma_decode_attention_prefix(odma_pool* pool, int32_t layer, const void*
         if (!workspace || workspace_bytes < w.bytes(1)) return ODMA_ERR_INVALID;
         splits = static_cast<int32_t>(std::min<int64_t>(splits, static_cast<int64_t>((workspace_bytes - w.kv_bytes) / (w.rows * w.row_bytes))));
     }
+    const bool tensor = prefix_on_tensor(pool), in_turn = tensor && splits >= 2 && n * (q_heads / pool->kv_heads) <= 128;
+    if (in_turn) splits &= ~1;
     cudaStream_t s = as_stream(stream);
     DecodeParams p;
     fill_decode_params(pool, layer, q, q_heads, tables, out, lse, &p);
@@ -1107,20 +1110,27 @@ int32_t odma_decode_attention_prefix(odma_pool* pool, int32_t layer, const void*
         pp.group = p.group;
         pp.head_dim = D;
         pp.splits = splits;
+        pp.in_turn = in_turn ? 1 : 0;
         pp.scale_log2 = p.scale_log2 * p.k_scale;
         pp.status = pool->d_status;
         pp.wait_limit_ns = p.wait_limit_ns;
         pp.k_row0 = static_cast<int32_t>(k_row0);
         pp.v_row0 = static_cast<int32_t>(k_row0 + pool->rows_per_array);
         ProfScope ps(pool, ODMA_K_DECODE, s);
+        TensorMaps ws_maps{};
         if (pool->dtype == ODMA_DTYPE_FP8_E4M3) {
             if (launch_dequant_prefix(k, v, pr->cap, prefix_len, w.pad, pool->kv_heads, D, workspace, s) != cudaSuccess)
                 return ODMA_ERR_CUDA;
             pp.k = workspace;
             pp.v = static_cast<uint8_t*>(workspace) + w.kv_bytes / 2;
             pp.head_rows = w.pad;
+            pp.k_row0 = 0;
+            pp.v_row0 = pool->kv_heads * w.pad;
+            if (make_tensor_maps(workspace, 2ll * pool->kv_heads * w.pad, D, 2, &ws_maps) != ODMA_OK) return ODMA_ERR_CUDA;
         }
-        if (launch_prefix(pp, fp32, s) != cudaSuccess) return ODMA_ERR_CUDA;
+        const TensorMaps& maps = pool->dtype == ODMA_DTYPE_FP8_E4M3 ? ws_maps : pool->maps;
+        const cudaError_t e = tensor ? launch_prefix_umma(maps.box[3], pp, s) : launch_prefix(pp, fp32, s);
+        if (e != cudaSuccess) return ODMA_ERR_CUDA;
     }
     {
         ProfScope ps(pool, ODMA_K_DECODE, s);

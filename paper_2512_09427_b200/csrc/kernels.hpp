@@ -185,7 +185,10 @@ struct PrefixParams {
     float scale_log2;
     uint32_t* status;
     int64_t wait_limit_ns;
-    int32_t k_row0, v_row0;     // rows of k and v in the tensor maps' array
+    // tensor-core kernel (prefix_umma.cu)
+    int32_t k_row0, v_row0;     // rows of k and v in the tensor map's array
+    int32_t in_turn;            // at most 128 rows per KV head: a block's two halves take its tiles in turn and
+                                // leave a partial result each (splits even)
 };
 struct MergePrefixParams {
     const int4* items;
@@ -200,8 +203,9 @@ struct MergePrefixParams {
     int32_t n, n_items, splits, q_heads, kv_heads, group, head_dim;
     float v_scale;              // of the prefix's partial results
 };
-int32_t prefix_splits(int32_t rows, int32_t kv_heads, int32_t len, int32_t sms, bool tensor);
+int32_t prefix_splits(int32_t rows, int32_t q_rows, int32_t kv_heads, int32_t len, int32_t sms, bool tensor);
 cudaError_t launch_prefix(const PrefixParams& p, bool fp32, cudaStream_t stream);
+cudaError_t launch_prefix_umma(const CUtensorMap& map, const PrefixParams& p, cudaStream_t stream);
 cudaError_t launch_dequant_prefix(const void* k, const void* v, int64_t head_rows, int32_t len, int32_t pad,
                                   int32_t kv_heads, int32_t head_dim, void* out, cudaStream_t stream);
 cudaError_t launch_merge_prefix(const MergePrefixParams& p, bool fp32, cudaStream_t stream);

@@ -9,6 +9,7 @@
 // requests' own parts come from the decode kernels, every piece left as a partial result.
 // merge_prefix_kernel folds both with the log-sum-exp rule and rounds once.
 //
+//  prefix_umma_kernel      tcgen05 tensor cores (prefix_umma.cu): 16- and 8-bit slabs, head_dim 64 and 128
 //  prefix_generic_kernel   plain ALUs, fp32 arithmetic: fp32 slabs, head_dim 32
 //  dequant_prefix_kernel   8-bit slabs: the prefix's codes as bf16 (exact: a code has 4 significant
 //                          bits); the scales stay outside, in the score factor and in the merge
@@ -232,31 +233,42 @@ template <typename T>
 cudaError_t launch_generic_t(const PrefixParams& p, cudaStream_t s) {
     const dim3 grid(static_cast<unsigned>((p.n * p.group + kRows - 1) / kRows), static_cast<unsigned>(p.kv_heads),
                     static_cast<unsigned>(p.splits));
-    switch (p.head_dim) {
-        case 32: prefix_generic_kernel<T, 1><<<grid, kWarps * 32, 0, s>>>(p); break;
-        case 64: prefix_generic_kernel<T, 2><<<grid, kWarps * 32, 0, s>>>(p); break;
-        case 128: prefix_generic_kernel<T, 4><<<grid, kWarps * 32, 0, s>>>(p); break;
-        default: return cudaErrorInvalidValue;
+    if (p.head_dim == 32) {
+        prefix_generic_kernel<T, 1><<<grid, kWarps * 32, 0, s>>>(p);
+    } else if constexpr (sizeof(T) == 4) {            // wider 16-bit rows: prefix_umma_kernel
+        if (p.head_dim == 64)
+            prefix_generic_kernel<T, 2><<<grid, kWarps * 32, 0, s>>>(p);
+        else if (p.head_dim == 128)
+            prefix_generic_kernel<T, 4><<<grid, kWarps * 32, 0, s>>>(p);
+        else
+            return cudaErrorInvalidValue;
+    } else {
+        return cudaErrorInvalidValue;
     }
     return cudaGetLastError();
 }
 
 }  // namespace
 
-int32_t prefix_splits(int32_t rows, int32_t kv_heads, int32_t len, int32_t sms, bool tensor) {
-    // Splits of the prefix's keys: enough blocks to fill the SMs, counted in waves, against what every
-    // split adds (a block's start-up and hand-over; a partial result to write and fold).
-    (void)tensor;
+// Splits of the prefix's keys, that is partial results per query row: the number that minimises
+// (waves of blocks) x (a block's time) + (the merge's time), in units of what a block of the tensor-core
+// kernel spends on one tile of 128 keys and 128 rows.  A block costs kBlockUnits more than its tiles
+// (tensor-memory and barrier set-up, queries, hand-over); a split costs every row a partial result.
+int32_t prefix_splits(int32_t rows, int32_t q_rows, int32_t kv_heads, int32_t len, int32_t sms, bool tensor) {
+    constexpr int64_t kBlockUnits = 6;
     const int64_t tiles = (len + kPrefixTile - 1) / kPrefixTile;
-    const int64_t blocks = static_cast<int64_t>((rows + kRows - 1) / kRows) * kv_heads, room = 4ll * sms;
+    const bool in_turn = tensor && rows <= 128;
+    // tensor cores: one block per SM, two tiles of 128 rows; plain ALUs: 8 rows, several blocks per SM
+    const int64_t blocks = kv_heads * static_cast<int64_t>(tensor ? (rows + 255) / 256 : (rows + kRows - 1) / kRows);
+    const int64_t room = tensor ? sms : 4ll * sms, per_tile = tensor ? (in_turn ? 1 : 2) : 4;
     int32_t best = 1;
     int64_t least = INT64_MAX;
-    for (int32_t s = 1; s <= std::min<int64_t>(tiles, kMaxPrefixSplits); ++s) {
-        const int64_t waves = (blocks * s + room - 1) / room;
-        const int64_t cost = waves * ((tiles + s - 1) / s * 4 + 2) + s / 4;
+    for (int32_t s = 1; s <= std::min<int64_t>(tiles, kMaxPrefixSplits); ++s) {      // s: blocks along the keys
+        const int64_t waves = (blocks * s + room - 1) / room, parts = in_turn ? 2 * s : s;
+        const int64_t cost = 16 * waves * ((tiles + s - 1) / s * per_tile + kBlockUnits) + parts * (2 + q_rows / 128);
         if (cost < least) {
             least = cost;
-            best = s;
+            best = static_cast<int32_t>(parts);
         }
     }
     return best;

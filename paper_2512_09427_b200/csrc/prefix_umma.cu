@@ -1,0 +1,424 @@
+// The prefix part of attention behind a shared prefix on the fifth-generation tensor cores (bf16 rows,
+// head_dim 64 or 128; 8-bit prefixes come here as bf16).  See prefix.cu for the operator.
+//
+// A block takes one KV head, one split of the prefix's keys and up to 256 query rows (row = request,
+// query head of the group).  With rows on the M side and 128 keys per tile
+//     S[128 x 128] = Q[128 x D] . K[128 x D]^T        Q, K from shared memory, K-major
+//     O[128 x D]  += P[128 x 128] . V[128 x D]        P from tensor memory, V MN-major
+// with S, P and O in tensor memory: S takes 128 columns, P (bf16) overwrites its first 64 once S has
+// been read, O takes D more.  Two such sets ("lanes") share the SM's tensor pipe: while one lane's
+// softmax runs, the other's products do.  More than 128 rows: the lanes hold two row tiles and use
+// every K and V tile twice; otherwise both hold the same rows and take the tiles in turn, each with
+// a partial result of its own.
+//
+// Warps 0-3 and 4-7: softmax of lane 0 and 1, a thread per row (a row's 128 scores are one tcgen05.ld
+// per 32 columns: no shuffles); warp 8: TMA producer; warp 9: issues all products, in the order
+// PV0(j) QK0(j+1) PV1(j) QK1(j+1), so S of a lane is only overwritten by a product issued after the
+// one that reads its P, and a full S tells that the lane's O is complete up to the tile before.
+//
+// The softmax keeps a reference m per row, raised only when a tile's maximum passes it by 2^8: P stays
+// below 256, which bf16 relative to the fp32 accumulator does not mind, and O is rescaled in tensor
+// memory only then.  P is rounded to bf16 for the product (half a step: 2^-9 to 2^-8 of a weight, random
+// in sign over the keys); sums, maxima and O are fp32.
+#include "odma.h"
+#include "tcgen05.cuh"
+
+namespace odma {
+namespace {
+
+using namespace dev;
+
+constexpr int kTile = kPrefixTile;                  // keys per tile
+constexpr int kM = 128;                             // rows per lane
+constexpr int kThreads = 320;
+constexpr int kProducerWarp = 8, kMmaWarp = 9;
+constexpr int kMaxStages = 8;
+constexpr float kRescaleAbove = 8.f;
+constexpr int kHalfBytes = kTile * 128;             // 64 elements of 128 rows
+// barriers
+constexpr int kBarFull = 0, kBarEmpty = kMaxStages, kBarQ = 2 * kMaxStages, kBarS = kBarQ + 2, kBarP = kBarS + 2,
+              kBarO = kBarP + 2, kBarDrain = kBarO + 2, kNumBars = kBarDrain + 1;
+
+template <int D>
+struct Config {
+    static constexpr int kHalves = D / 64;
+    static constexpr int kTileBytes = kHalves * kHalfBytes;      // of K, of V, and of a lane's Q
+    static constexpr int kStages = D == 128 ? 5 : 8;
+    static constexpr int kSmem = (2 + kStages) * kTileBytes + kNumBars * 8 + 64 + 1024;
+};
+
+// D[tmem] (+)= A[tmem] . B[smem]
+__device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %5, %5, %5}, p;\n\t}" ::"r"(d_tmem),
+        "r"(a_tmem), "l"(b), "r"(idesc), "r"(accumulate), "r"(0u)
+        : "memory");
+}
+
+// 32 columns of the thread's own row (tensor-memory lane = 32 * (warp mod 4) + lane).
+__device__ __forceinline__ void tmem_ld_row32(uint32_t addr, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_st_row32(uint32_t addr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+        "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(addr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
+        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
+        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+
+__device__ __forceinline__ void tmem_st_row16(uint32_t addr, const uint32_t* r) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p) {
+    using Cfg = Config<D>;
+    constexpr int STAGES = Cfg::kStages;
+    constexpr uint32_t IDESC_QK = umma_idesc(kM, kTile, false), IDESC_PV = umma_idesc(kM, D, true);
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+    uint8_t* qbuf = smem;
+    uint8_t* kv = qbuf + 2 * Cfg::kTileBytes;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(kv + STAGES * Cfg::kTileBytes);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + kNumBars);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(const_cast<int*>(abort_flag) + 1);
+    const uint32_t bar0 = smem_u32(bars);
+    auto bar = [&](int i) { return bar0 + 8u * static_cast<uint32_t>(i); };
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int64_t limit = p.wait_limit_ns;
+
+    // the block's work
+    const int head = blockIdx.y;
+    const int rows = p.n * p.group, r0 = blockIdx.x * 2 * kM;
+    const bool in_turn = p.in_turn != 0;             // both lanes on the same rows, tiles in turn
+    const bool lane1 = in_turn || r0 + kM < rows;    // is there a second lane?
+    const int blocks = in_turn ? p.splits >> 1 : p.splits;      // splits of the keys over the blocks
+    const int all_tiles = (p.len + kTile - 1) / kTile;
+    const int t0 = static_cast<int>(static_cast<int64_t>(all_tiles) * blockIdx.z / blocks);
+    const int t1 = static_cast<int>(static_cast<int64_t>(all_tiles) * (blockIdx.z + 1) / blocks);
+    const int tiles = t1 - t0;
+    const int ahead = in_turn ? 2 : 1;               // K tiles requested before the first V tile
+
+    if (tid < kNumBars) {
+        const bool many = (tid >= kBarQ && tid < kBarS) || (tid >= kBarP && tid < kBarO);   // a lane's 128 threads
+        mbar_init(bar(tid), many ? 128u : 1u);
+    }
+    if (tid == 0) {
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == kMmaWarp) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    const uint32_t kv_u32 = smem_u32(kv), q_u32 = smem_u32(qbuf);
+    bool ok = true;
+
+    if (warp == kProducerWarp) {
+        // ------------------------------------------------------------------ producer
+        // Ring order: the first `ahead` K tiles, then V(j), K(j + ahead) for each j.
+        if (lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map)) : "memory");
+        uint32_t issued = 0;
+        auto load = [&](bool is_v, int t) {
+            const uint32_t stage = issued % STAGES, use = issued / STAGES;
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(kBarEmpty + stage), (use & 1u) ^ 1u, abort_flag, p.status, limit));
+            if (!ok) return;
+            // a tile is two boxes of 64 rows per 128-byte column block; the prefix's last tile may need one only
+            const int boxes = p.len - (t0 + t) * kTile > 64 ? 2 : 1;
+            if (lane == 0) mbar_expect_tx(bar(kBarFull + stage), static_cast<uint32_t>(boxes * Cfg::kHalves) * 8192u);
+            __syncwarp();
+            const int h = lane >> 1, b = lane & 1;
+            if (h < Cfg::kHalves && b < boxes)
+                tma_load_2d(kv_u32 + stage * Cfg::kTileBytes + h * kHalfBytes + b * 8192, &map, h * 64,
+                            static_cast<int32_t>((is_v ? p.v_row0 : p.k_row0) + head * p.head_rows + (t0 + t) * kTile + b * 64),
+                            bar(kBarFull + stage));
+            ++issued;
+        };
+        for (int t = 0; t < min(ahead, tiles) && ok; ++t) load(false, t);
+        for (int t = 0; t < tiles && ok; ++t) {
+            load(true, t);
+            if (ok && t + ahead < tiles) load(false, t + ahead);
+        }
+        if (lane == 0 && (!ok || *abort_flag)) {
+            // something timed out: wait (bounded) for the loads in flight before shared memory is given up
+            for (uint32_t i = issued > STAGES ? issued - STAGES : 0; i < issued; ++i)
+                mbar_wait_slow(bar(kBarFull + i % STAGES), (i / STAGES) & 1u, nullptr, p.status, limit / 4 + 1);
+        }
+    } else if (warp == kMmaWarp) {
+        // ------------------------------------------------------------------ products
+        uint32_t elected;
+        asm volatile("{\n\t.reg .pred P;\n\telect.sync _|P, 0xFFFFFFFF;\n\tselp.b32 %0, 1, 0, P;\n\t}" : "=r"(elected));
+        uint32_t used = 0;                           // ring position
+        auto wait_tile = [&]() {                     // the next tile of the ring; its stage
+            const uint32_t stage = used % STAGES;
+            ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait(bar(kBarFull + stage), (used / STAGES) & 1u, abort_flag, p.status, limit));
+            tc_fence_after();
+            ++used;
+            return stage;
+        };
+        auto wait_bar = [&](int b, uint32_t parity) {
+            ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait_spin(bar(b), parity, abort_flag, p.status, limit));
+            tc_fence_after();
+        };
+        auto first = [&](int L, uint32_t stage) {    // S of lane L from the K tile in `stage`
+            const uint32_t qb = q_u32 + (in_turn ? 0u : static_cast<uint32_t>(L) * Cfg::kTileBytes), kb = kv_u32 + stage * Cfg::kTileBytes;
+            if (ok && elected) {
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks)
+                    umma<false>(tmem + static_cast<uint32_t>(L) * 256u, smem_desc(qb + (ks >> 2) * kHalfBytes + (ks & 3) * 32, 16, 1024),
+                                smem_desc(kb + (ks >> 2) * kHalfBytes + (ks & 3) * 32, 16, 1024), IDESC_QK, ks > 0 ? 1u : 0u);
+                umma_commit(bar(kBarS + L));
+            }
+            __syncwarp();
+        };
+        auto second = [&](int L, int t, uint32_t stage, bool start, bool last) {     // O of lane L += P V
+            const uint32_t base = tmem + static_cast<uint32_t>(L) * 256u, vb = kv_u32 + stage * Cfg::kTileBytes;
+            const int keys = min(kTile, p.len - (t0 + t) * kTile), steps = (keys + 15) >> 4;
+            if (ok && elected) {
+                for (int ks = 0; ks < steps; ++ks)
+                    umma_ts(base + 128u, base + static_cast<uint32_t>(ks) * 8u, smem_desc(vb + ks * 2048, kHalfBytes, 1024), IDESC_PV,
+                            (start && ks == 0) ? 0u : 1u);
+                if (last) umma_commit(bar(kBarO + L));
+            }
+            __syncwarp();
+        };
+        auto release = [&](uint32_t stage) {
+            if (ok && elected) umma_commit(bar(kBarEmpty + stage));
+            __syncwarp();
+        };
+        // value rows between the prefix's end and the next multiple of 16: whatever the slab holds there,
+        // and 0 times a NaN would not be 0
+        auto clear_tail = [&](int t, uint32_t stage) {
+            const int keys = min(kTile, p.len - (t0 + t) * kTile), end = (keys + 15) & ~15;
+            if (keys == end || !ok) return;
+            uint8_t* vb = kv + stage * Cfg::kTileBytes;
+            for (int i = lane; i < (end - keys) * 8 * Cfg::kHalves; i += 32) {
+                const int row = keys + i / (8 * Cfg::kHalves), c = i % (8 * Cfg::kHalves);
+                *reinterpret_cast<uint4*>(vb + (c >> 3) * kHalfBytes + row * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+            }
+            fence_proxy_async();
+            __syncwarp();
+        };
+        wait_bar(kBarQ, 0);
+        if (!in_turn) {
+            if (lane1) wait_bar(kBarQ + 1, 0);
+            uint32_t ks = wait_tile();
+            first(0, ks);
+            if (lane1) first(1, ks);
+            release(ks);
+            for (int t = 0; t < tiles && ok; ++t) {
+                const bool last = t + 1 == tiles;
+                const uint32_t vs = wait_tile();
+                clear_tail(t, vs);
+                wait_bar(kBarP, t & 1u);
+                second(0, t, vs, t == 0, last);
+                if (!last) {
+                    ks = wait_tile();
+                    first(0, ks);
+                }
+                if (lane1) {
+                    wait_bar(kBarP + 1, t & 1u);
+                    second(1, t, vs, t == 0, last);
+                }
+                release(vs);
+                if (!last) {
+                    if (lane1) first(1, ks);
+                    release(ks);
+                }
+            }
+        } else {
+            for (int t = 0; t < min(2, tiles) && ok; ++t) {
+                const uint32_t ks = wait_tile();
+                first(t, ks);
+                release(ks);
+            }
+            for (int t = 0; t < tiles && ok; ++t) {
+                const int L = t & 1;
+                const uint32_t vs = wait_tile();
+                clear_tail(t, vs);
+                wait_bar(kBarP + L, static_cast<uint32_t>(t >> 1) & 1u);
+                second(L, t, vs, t < 2, t + 2 >= tiles);
+                release(vs);
+                if (t + 2 < tiles) {
+                    const uint32_t ks = wait_tile();
+                    first(L, ks);
+                    release(ks);
+                }
+            }
+        }
+        // nothing may still be running when tensor memory is given back
+        if (elected) umma_commit(bar(kBarDrain));
+        __syncwarp();
+        mbar_wait_slow(bar(kBarDrain), 0, nullptr, p.status, limit / 4 + 1);
+    } else {
+        // ------------------------------------------------------------------ softmax
+        const int L = warp >> 2;
+        const int row = (warp & 3) * 32 + lane;      // of the lane's tile
+        const int g_row = r0 + (in_turn ? 0 : L * kM) + row;
+        auto out_row = [&](int r) { return static_cast<int64_t>(r / p.group) * p.q_heads + head * p.group + r % p.group; };
+        if (L == 0 || (lane1 && !in_turn)) {
+            // queries to shared memory in the swizzled order; rows behind the last are zero
+            constexpr int CH = D / 8;                // 16-byte chunks per row
+            const uint4* q = static_cast<const uint4*>(p.q);
+            uint8_t* dst = qbuf + L * Cfg::kTileBytes;
+#pragma unroll 4
+            for (int i = tid & 127; i < kM * CH; i += 128) {
+                const int r = i / CH, c = i - r * CH, g = r0 + L * kM + r;
+                uint4 v = make_uint4(0u, 0u, 0u, 0u);
+                if (g < rows) v = __ldg(q + out_row(g) * CH + c);
+                *reinterpret_cast<uint4*>(dst + (c >> 3) * kHalfBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v;
+            }
+            fence_proxy_async();
+            mbar_arrive(bar(kBarQ + L));
+        }
+        const uint32_t t_s = tmem + (static_cast<uint32_t>(warp & 3) << 21) + static_cast<uint32_t>(L) * 256u, t_o = t_s + 128u;
+        const float scale = p.scale_log2;
+        float m = -INFINITY, l = 0.f;                // reference (log2 units) and sum
+        const int first_t = in_turn ? L : 0, step = in_turn ? 2 : 1;
+        const bool active = L == 0 || lane1;
+        uint32_t done = 0;                           // tiles of this lane so far
+        for (int t = first_t; t < tiles && active; t += step, ++done) {
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait_spin(bar(kBarS + L), done & 1u, abort_flag, p.status, limit));
+            if (!ok) break;
+            tc_fence_after();
+            uint32_t s[kTile];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_ld_row32(t_s + 32u * c, s + 32 * c);
+            tmem_wait_ld();
+            const int keys = p.len - (t0 + t) * kTile;
+            if (keys < kTile) {
+#pragma unroll
+                for (int i = 0; i < kTile; ++i)
+                    if (i >= keys) s[i] = 0xFF800000u;           // -inf
+            }
+            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int i = 0; i < kTile; i += 4)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], __uint_as_float(s[i + k]));
+            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
+            // raise the reference: the first tile's maximum, later only past 2^8 times the reference
+            const bool raise = done == 0 ? top > m : top > m + kRescaleAbove;
+            const float before = m;
+            if (raise) m = top;
+            if (done > 0 && __any_sync(0xFFFFFFFFu, raise)) {
+                const float f = raise ? fast_exp2(before - m) : 1.f;
+                l *= f;
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                    uint32_t o[32];
+                    tmem_ld_row32(t_o + 32u * c, o);
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                    tmem_st_row32(t_o + 32u * c, o);
+                }
+            }
+            const float ref = m == -INFINITY ? 0.f : m;          // every score so far is -inf: weights 0, not NaN
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                uint32_t pk[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float a = fast_exp2(fmaf(__uint_as_float(s[32 * c + 2 * i]), scale, -ref));
+                    const float b = fast_exp2(fmaf(__uint_as_float(s[32 * c + 2 * i + 1]), scale, -ref));
+                    sum[(2 * i) & 3] += a;
+                    sum[(2 * i + 1) & 3] += b;
+                    pk[i] = pack_bf16(a, b);
+                }
+                tmem_st_row16(t_s + 16u * c, pk);
+            }
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            tmem_wait_st();
+            tc_fence_before();
+            mbar_arrive(bar(kBarP + L));
+        }
+        // the lane's result
+        const int part = in_turn ? 2 * blockIdx.z + L : blockIdx.z;
+        const int64_t at = static_cast<int64_t>(part) * p.n * p.q_heads + (g_row < rows ? out_row(g_row) : 0);
+        const bool mine = active && g_row < rows;
+        if (done > 0 && ok) {
+            ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(kBarO + L), 0, abort_flag, p.status, limit));
+            tc_fence_after();
+        }
+        if (ok) {
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t o[32];
+                if (done > 0) {
+                    tmem_ld_row32(t_o + 32u * c, o);
+                    tmem_wait_ld();
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) o[i] = 0u;
+                }
+                if (mine) {
+                    uint4* dst = reinterpret_cast<uint4*>(p.part_o + at * D + 32 * c);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) dst[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+                }
+            }
+            if (mine) *reinterpret_cast<float2*>(p.part_ml + 2 * at) = make_float2(m, l);
+        }
+    }
+    // ---- tear-down: every role comes here, on every path, and tensor memory is given back
+    if (!ok) *abort_flag = 1;
+    tc_fence_before();
+    __syncthreads();
+    if (warp == kMmaWarp) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    }
+}
+
+template <int D>
+cudaError_t launch_t(const CUtensorMap& map, const PrefixParams& p, cudaStream_t stream) {
+    static bool configured[64] = {false};             // the opt-in to large shared memory is per device
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    if (!configured[dev]) {
+        e = cudaFuncSetAttribute(prefix_umma_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Config<D>::kSmem);
+        if (e != cudaSuccess) return e;
+        configured[dev] = true;
+    }
+    const int rows = p.n * p.group;
+    const dim3 grid(static_cast<unsigned>((rows + 2 * kM - 1) / (2 * kM)), static_cast<unsigned>(p.kv_heads),
+                    static_cast<unsigned>(p.in_turn ? p.splits / 2 : p.splits));
+    prefix_umma_kernel<D><<<grid, kThreads, Config<D>::kSmem, stream>>>(map, p);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_prefix_umma(const CUtensorMap& map, const PrefixParams& p, cudaStream_t stream) {
+    if (p.splits < 1 || p.len < 1) return cudaSuccess;
+    return p.head_dim == 128 ? launch_t<128>(map, p, stream) : launch_t<64>(map, p, stream);
+}
+
+}  // namespace odma
