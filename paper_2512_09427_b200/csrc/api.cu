@@ -1041,9 +1041,9 @@ PrefixSpace prefix_space(const odma_pool* pool, int32_t q_heads, int32_t n, int3
 // Does the prefix's product run on the tensor cores?  (Asked of bookkeeping-only pools too.)
 bool prefix_on_tensor(const odma_pool* pool) { return pool->dtype != ODMA_DTYPE_F32 && tc_supported(pool->head_dim, 1); }
 
-int32_t prefix_splits_of(const odma_pool* pool, int32_t q_heads, int32_t n, int32_t len) {
-    return len < 1 ? 0 : prefix_splits(n * (q_heads / pool->kv_heads), n * q_heads, pool->kv_heads, len, pool->plan_ctas,
-                                       prefix_on_tensor(pool));
+PrefixSplit prefix_split_of(const odma_pool* pool, int32_t q_heads, int32_t n, int32_t len) {
+    if (len < 1) return PrefixSplit{0, 0};
+    return prefix_split(n * (q_heads / pool->kv_heads), n * q_heads, pool->kv_heads, len, pool->plan_ctas, prefix_on_tensor(pool));
 }
 
 bool prefix_shape_ok(const odma_pool* pool, int32_t q_heads, int32_t n, int32_t len) {
@@ -1059,7 +1059,7 @@ extern "C" {
 
 uint64_t odma_prefix_workspace_bytes(const odma_pool* pool, int32_t q_heads, int32_t n, int32_t prefix_len) {
     if (!pool || !prefix_shape_ok(pool, q_heads, n, prefix_len)) return 0;
-    const uint64_t b = prefix_space(pool, q_heads, n, prefix_len).bytes(prefix_splits_of(pool, q_heads, n, prefix_len));
+    const uint64_t b = prefix_space(pool, q_heads, n, prefix_len).bytes(prefix_split_of(pool, q_heads, n, prefix_len).splits);
     return std::max<uint64_t>((b + 255) / 256 * 256, 256);
 }
 
@@ -1076,12 +1076,13 @@ int32_t odma_decode_attention_prefix(odma_pool* pool, int32_t layer, const void*
     const int32_t D = pool->head_dim, n = tables->n;
     // as many splits of the prefix as are worth while, and as fit
     const PrefixSpace w = prefix_space(pool, q_heads, n, prefix_len);
-    int32_t splits = prefix_splits_of(pool, q_heads, n, prefix_len);
+    const PrefixSplit plan = prefix_split_of(pool, q_heads, n, prefix_len);
+    int32_t splits = plan.splits;
     if (splits > 0) {
         if (!workspace || workspace_bytes < w.bytes(1)) return ODMA_ERR_INVALID;
         splits = static_cast<int32_t>(std::min<int64_t>(splits, static_cast<int64_t>((workspace_bytes - w.kv_bytes) / (w.rows * w.row_bytes))));
     }
-    const bool tensor = prefix_on_tensor(pool), in_turn = tensor && splits >= 2 && n * (q_heads / pool->kv_heads) <= 128;
+    const bool tensor = prefix_on_tensor(pool), in_turn = plan.in_turn && splits >= 2;
     if (in_turn) splits &= ~1;
     cudaStream_t s = as_stream(stream);
     DecodeParams p;

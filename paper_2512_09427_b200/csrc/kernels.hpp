@@ -203,7 +203,11 @@ struct MergePrefixParams {
     int32_t n, n_items, splits, q_heads, kv_heads, group, head_dim;
     float v_scale;              // of the prefix's partial results
 };
-int32_t prefix_splits(int32_t rows, int32_t q_rows, int32_t kv_heads, int32_t len, int32_t sms, bool tensor);
+struct PrefixSplit {
+    int32_t splits;             // partial results per query row
+    int32_t in_turn;            // see PrefixParams
+};
+PrefixSplit prefix_split(int32_t rows, int32_t q_rows, int32_t kv_heads, int32_t len, int32_t sms, bool tensor);
 cudaError_t launch_prefix(const PrefixParams& p, bool fp32, cudaStream_t stream);
 cudaError_t launch_prefix_umma(const CUtensorMap& map, const PrefixParams& p, cudaStream_t stream);
 cudaError_t launch_dequant_prefix(const void* k, const void* v, int64_t head_rows, int32_t len, int32_t pad,

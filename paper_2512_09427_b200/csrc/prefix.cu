@@ -26,6 +26,7 @@ using namespace dev;
 
 constexpr int kRows = 8;            // query rows a block of the generic kernel carries
 constexpr int kWarps = 4;
+constexpr int kMergeWarps = 8;
 
 __device__ __forceinline__ void unpack16(const uint4& v, float (&x)[4], float) {
     x[0] = __uint_as_float(v.x);
@@ -43,6 +44,26 @@ __device__ __forceinline__ void unpack16(const uint4& v, float (&x)[8], __nv_bfl
 }
 __device__ __forceinline__ float as_float(float x) { return x; }
 __device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162float(x); }
+
+__device__ __forceinline__ void load_row(const float* p, float (&x)[1]) { x[0] = __ldcg(p); }
+__device__ __forceinline__ void load_row(const float* p, float (&x)[2]) {
+    const float2 v = __ldcg(reinterpret_cast<const float2*>(p));
+    x[0] = v.x;
+    x[1] = v.y;
+}
+__device__ __forceinline__ void load_row(const float* p, float (&x)[4]) {
+    const float4 v = ldcg4(p);
+    x[0] = v.x;
+    x[1] = v.y;
+    x[2] = v.z;
+    x[3] = v.w;
+}
+__device__ __forceinline__ void store_row(float* p, const float (&x)[1]) { *p = x[0]; }
+__device__ __forceinline__ void store_row(float* p, const float (&x)[2]) { *reinterpret_cast<float2*>(p) = make_float2(x[0], x[1]); }
+__device__ __forceinline__ void store_row(float* p, const float (&x)[4]) { store4(p, x[0], x[1], x[2], x[3]); }
+__device__ __forceinline__ void store_row(__nv_bfloat16* p, const float (&x)[1]) { *p = __float2bfloat16_rn(x[0]); }
+__device__ __forceinline__ void store_row(__nv_bfloat16* p, const float (&x)[2]) { *reinterpret_cast<uint32_t*>(p) = pack_bf16(x[0], x[1]); }
+__device__ __forceinline__ void store_row(__nv_bfloat16* p, const float (&x)[4]) { store4(p, x[0], x[1], x[2], x[3]); }
 
 // Keys [first, last) of split s: the prefix's tiles of 128 keys dealt evenly.
 __device__ __forceinline__ void split_range(const PrefixParams& p, int s, int& first, int& last) {
@@ -181,10 +202,15 @@ __global__ void __launch_bounds__(256) dequant_prefix_kernel(const uint8_t* k, c
     }
 }
 
-// Blocks [0, n_items): the stream that begins with this item.  Blocks behind them: the requests, for
-// those without a token of their own.
-template <typename T>
-__global__ void __launch_bounds__(128) merge_prefix_kernel(const MergePrefixParams p) {
+// Blocks [0, n_items): the stream that begins with this item, a warp per query head.  Blocks behind
+// them: the requests, for those without a token of their own.  A row's parts are its own pieces and then
+// the prefix's splits, in that order.  32 at a time: a lane fetches one part's (m, l), the warp finds
+// the maximum and every part's factor 2^(m - M), and the rows are added up with all loads independent
+// of one another (folded one after the other, 15 parts took 13 us; a chain of L2 round trips).
+template <typename T, int V>        // head_dim = 32 * V
+__global__ void __launch_bounds__(kMergeWarps * 32) merge_prefix_kernel(const MergePrefixParams p) {
+    constexpr int D = 32 * V;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     int req, head, heads = 1, slot0 = 0, pieces = 0;
     if (static_cast<int>(blockIdx.x) < p.n_items) {
         const int4 a = __ldg(p.items + 2 * blockIdx.x), b = __ldg(p.items + 2 * blockIdx.x + 1);
@@ -199,33 +225,48 @@ __global__ void __launch_bounds__(128) merge_prefix_kernel(const MergePrefixPara
         head = 0;
         heads = p.kv_heads;
     }
-    const int D = p.head_dim, per_row = D >> 2;
+    const int lane = threadIdx.x & 31;
     const int64_t split_rows = static_cast<int64_t>(p.n) * p.q_heads;
-    for (int idx = threadIdx.x; idx < heads * p.group * per_row; idx += blockDim.x) {
-        const int g = idx / per_row, d0 = (idx - g * per_row) * 4;
+    for (int g = threadIdx.x >> 5; g < heads * p.group; g += kMergeWarps) {
         const int64_t row = static_cast<int64_t>(req) * p.q_heads + head * p.group + g;
-        float M = -INFINITY, L = 0.f;
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 2
-        for (int s = 0; s < pieces; ++s) {
-            const int64_t at = static_cast<int64_t>(slot0 + s) * p.group + g;
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(p.own_ml + 2 * at));
-            lse_fold(M, L, acc, ml.x, ml.y, ldcg4(p.own_o + at * D + d0));
-        }
-#pragma unroll 4
-        for (int s = 0; s < p.splits; ++s) {
-            const int64_t at = s * split_rows + row;
-            const float2 ml = __ldcg(reinterpret_cast<const float2*>(p.part_ml + 2 * at));
-            float4 x = ldcg4(p.part_o + at * D + d0);
-            x.x *= p.v_scale;
-            x.y *= p.v_scale;
-            x.z *= p.v_scale;
-            x.w *= p.v_scale;
-            lse_fold(M, L, acc, ml.x, ml.y, x);
+        const int64_t own_row = static_cast<int64_t>(slot0) * p.group + g;
+        float M = -INFINITY, L = 0.f, acc[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) acc[i] = 0.f;
+        const int parts = pieces + p.splits;
+        for (int s0 = 0; s0 < parts; s0 += 32) {
+            const int s = s0 + lane, count = min(32, parts - s0);
+            float2 ml = make_float2(-INFINITY, 0.f);
+            if (s < parts) ml = __ldcg(reinterpret_cast<const float2*>(s < pieces ? p.own_ml + 2 * (own_row + static_cast<int64_t>(s) * p.group)
+                                                                                  : p.part_ml + 2 * ((s - pieces) * split_rows + row)));
+            float top = fmaxf(M, ml.x);
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
+            const float e = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - top), old = M == -INFINITY ? 0.f : fast_exp2(M - top);
+            float sum = ml.y * e;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+            L = fmaf(L, old, sum);
+            M = top;
+#pragma unroll
+            for (int i = 0; i < V; ++i) acc[i] *= old;
+            const float f = s < pieces ? e : e * p.v_scale;
+#pragma unroll 8
+            for (int k = 0; k < count; ++k) {
+                const float w = __shfl_sync(0xFFFFFFFFu, f, k);
+                const float* src = s0 + k < pieces ? p.own_o + (own_row + static_cast<int64_t>(s0 + k) * p.group) * D
+                                                   : p.part_o + ((s0 + k - pieces) * split_rows + row) * D;
+                float x[V];
+                load_row(src + lane * V, x);
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[i] = fmaf(x[i], w, acc[i]);
+            }
         }
         const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);      // no key at all: zeros
-        store4(static_cast<T*>(p.out) + row * D + d0, acc.x * inv, acc.y * inv, acc.z * inv, acc.w * inv);
-        if (d0 == 0 && p.lse) p.lse[row] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+#pragma unroll
+        for (int i = 0; i < V; ++i) acc[i] *= inv;
+        store_row(static_cast<T*>(p.out) + row * D + lane * V, acc);
+        if (lane == 0 && p.lse) p.lse[row] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
     }
 }
 
@@ -250,25 +291,28 @@ cudaError_t launch_generic_t(const PrefixParams& p, cudaStream_t s) {
 
 }  // namespace
 
-// Splits of the prefix's keys, that is partial results per query row: the number that minimises
-// (waves of blocks) x (a block's time) + (the merge's time), in units of what a block of the tensor-core
-// kernel spends on one tile of 128 keys and 128 rows.  A block costs kBlockUnits more than its tiles
-// (tensor-memory and barrier set-up, queries, hand-over); a split costs every row a partial result.
-int32_t prefix_splits(int32_t rows, int32_t q_rows, int32_t kv_heads, int32_t len, int32_t sms, bool tensor) {
+// Blocks along the prefix's keys: the number that minimises (waves of blocks) x (a block's time) + (the
+// merge's time), in sixteenths of what a block of the tensor-core kernel spends on one tile of 128 keys
+// and 128 rows.  A block costs kBlockUnits tiles more than its own (tensor-memory and barrier set-up,
+// queries, hand-over); every partial result costs its row a write and a read.
+PrefixSplit prefix_split(int32_t rows, int32_t q_rows, int32_t kv_heads, int32_t len, int32_t sms, bool tensor) {
     constexpr int64_t kBlockUnits = 6;
     const int64_t tiles = (len + kPrefixTile - 1) / kPrefixTile;
-    const bool in_turn = tensor && rows <= 128;
     // tensor cores: one block per SM, two tiles of 128 rows; plain ALUs: 8 rows, several blocks per SM
     const int64_t blocks = kv_heads * static_cast<int64_t>(tensor ? (rows + 255) / 256 : (rows + kRows - 1) / kRows);
-    const int64_t room = tensor ? sms : 4ll * sms, per_tile = tensor ? (in_turn ? 1 : 2) : 4;
-    int32_t best = 1;
+    const int64_t room = tensor ? sms : 4ll * sms;
+    PrefixSplit best{1, 0};
     int64_t least = INT64_MAX;
-    for (int32_t s = 1; s <= std::min<int64_t>(tiles, kMaxPrefixSplits); ++s) {      // s: blocks along the keys
-        const int64_t waves = (blocks * s + room - 1) / room, parts = in_turn ? 2 * s : s;
-        const int64_t cost = 16 * waves * ((tiles + s - 1) / s * per_tile + kBlockUnits) + parts * (2 + q_rows / 128);
-        if (cost < least) {
-            least = cost;
-            best = static_cast<int32_t>(parts);
+    for (int32_t s = 1; s <= std::min<int64_t>(tiles, kMaxPrefixSplits); ++s) {
+        const int64_t waves = (blocks * s + room - 1) / room, each = (tiles + s - 1) / s;
+        for (int32_t turn = 0; turn <= (tensor && rows <= 128 && tiles >= 2 * s ? 1 : 0); ++turn) {
+            // one row tile alone waits for itself (its softmax and its products in turn): twice a tile's time
+            const int64_t work = !tensor ? 4 * each : turn ? each : 2 * each, parts = turn ? 2 * s : s;
+            const int64_t cost = 16 * waves * (work + kBlockUnits) + parts * (2 + q_rows / 128);
+            if (cost < least) {
+                least = cost;
+                best = PrefixSplit{static_cast<int32_t>(parts), turn};
+            }
         }
     }
     return best;
@@ -288,13 +332,30 @@ cudaError_t launch_dequant_prefix(const void* k, const void* v, int64_t head_row
     return cudaGetLastError();
 }
 
+namespace {
+// Launched with programmatic stream serialization: the blocks are there when the kernel ahead ends.
+template <typename T, int V>
+cudaError_t launch_merge_t(const MergePrefixParams& p, cudaStream_t stream) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(p.n_items + p.n));
+    cfg.blockDim = dim3(kMergeWarps * 32);
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, merge_prefix_kernel<T, V>, p);
+}
+}  // namespace
+
 cudaError_t launch_merge_prefix(const MergePrefixParams& p, bool fp32, cudaStream_t stream) {
-    const int grid = p.n_items + p.n;
-    if (fp32)
-        merge_prefix_kernel<float><<<grid, 128, 0, stream>>>(p);
-    else
-        merge_prefix_kernel<__nv_bfloat16><<<grid, 128, 0, stream>>>(p);
-    return cudaGetLastError();
+    switch (p.head_dim) {
+        case 32: return fp32 ? launch_merge_t<float, 1>(p, stream) : launch_merge_t<__nv_bfloat16, 1>(p, stream);
+        case 64: return fp32 ? launch_merge_t<float, 2>(p, stream) : launch_merge_t<__nv_bfloat16, 2>(p, stream);
+        case 128: return fp32 ? launch_merge_t<float, 4>(p, stream) : launch_merge_t<__nv_bfloat16, 4>(p, stream);
+    }
+    return cudaErrorInvalidValue;
 }
 
 }  // namespace odma

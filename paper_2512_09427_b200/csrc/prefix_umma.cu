@@ -68,23 +68,67 @@ __device__ __forceinline__ void tmem_ld_row32(uint32_t addr, uint32_t* r) {
         : "r"(addr)
         : "memory");
 }
-__device__ __forceinline__ void tmem_st_row32(uint32_t addr, const uint32_t* r) {
+__device__ __forceinline__ void tmem_ld_row16(uint32_t addr, uint32_t* r) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
-        "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(addr),
-        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
-        "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]),
-        "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]),
-        "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr)
         : "memory");
 }
-
 __device__ __forceinline__ void tmem_st_row16(uint32_t addr, const uint32_t* r) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr),
         "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
         "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
+}
+
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(const float2& a, const float2& b, const float2& c) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, z, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\t"
+        "fma.rn.f32x2 w, x, y, z;\n\tmov.b64 {%0, %1}, w;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return d;
+}
+__device__ __forceinline__ float2 add2(const float2& a, const float2& b) {
+    float2 d;
+    asm("{\n\t.reg .b64 x, y, w;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\t"
+        "add.rn.f32x2 w, x, y;\n\tmov.b64 {%0, %1}, w;\n\t}"
+        : "=f"(d.x), "=f"(d.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+
+__device__ __forceinline__ float row_max(const uint32_t (&s)[kTile]) {
+    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+    for (int i = 0; i < kTile; i += 8)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) mx[k] = fmaxf(fmaxf(mx[k], __uint_as_float(s[i + 2 * k])), __uint_as_float(s[i + 2 * k + 1]));
+    return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
+}
+
+// The row's weights 2^(s * scale - m), rounded to bf16, to tensor memory; their sum (unrounded).
+__device__ __forceinline__ float row_weights(const uint32_t (&s)[kTile], float scale, float m, uint32_t t_p) {
+    const float ref = m == -INFINITY ? 0.f : m;     // every score so far is -inf: weights 0, not NaN
+    const float2 sc = make_float2(scale, scale), neg = make_float2(-ref, -ref);
+    float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        uint32_t pk[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            float2 x = fma2(make_float2(__uint_as_float(s[32 * c + 2 * i]), __uint_as_float(s[32 * c + 2 * i + 1])), sc, neg);
+            x = make_float2(fast_exp2(x.x), fast_exp2(x.y));
+            sum[i & 1] = add2(sum[i & 1], x);
+            pk[i] = pack_bf16(x.x, x.y);
+        }
+        tmem_st_row16(t_p + 16u * c, pk);
+    }
+    return (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
 }
 
 template <int D>
@@ -136,7 +180,6 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
     const uint32_t tmem = *tmem_slot;
     const uint32_t kv_u32 = smem_u32(kv), q_u32 = smem_u32(qbuf);
     bool ok = true;
-
     if (warp == kProducerWarp) {
         // ------------------------------------------------------------------ producer
         // Ring order: the first `ahead` K tiles, then V(j), K(j + ahead) for each j.
@@ -284,12 +327,18 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
             constexpr int CH = D / 8;                // 16-byte chunks per row
             const uint4* q = static_cast<const uint4*>(p.q);
             uint8_t* dst = qbuf + L * Cfg::kTileBytes;
-#pragma unroll 4
-            for (int i = tid & 127; i < kM * CH; i += 128) {
-                const int r = i / CH, c = i - r * CH, g = r0 + L * kM + r;
-                uint4 v = make_uint4(0u, 0u, 0u, 0u);
-                if (g < rows) v = __ldg(q + out_row(g) * CH + c);
-                *reinterpret_cast<uint4*>(dst + (c >> 3) * kHalfBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v;
+            uint4 v[CH];
+            const int c = tid % CH, rr = (tid & 127) / CH;       // chunk, first of the thread's rows
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {           // all loads before the first store
+                const int g = r0 + L * kM + rr + i * (128 / CH);
+                v[i] = make_uint4(0u, 0u, 0u, 0u);
+                if (g < rows) v[i] = __ldg(q + out_row(g) * CH + c);
+            }
+#pragma unroll
+            for (int i = 0; i < CH; ++i) {
+                const int r = rr + i * (128 / CH);
+                *reinterpret_cast<uint4*>(dst + (c >> 3) * kHalfBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v[i];
             }
             fence_proxy_async();
             mbar_arrive(bar(kBarQ + L));
@@ -306,7 +355,7 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
             tc_fence_after();
             uint32_t s[kTile];
 #pragma unroll
-            for (int c = 0; c < 4; ++c) tmem_ld_row32(t_s + 32u * c, s + 32 * c);
+            for (int c = 0; c < 8; ++c) tmem_ld_row16(t_s + 16u * c, s + 16 * c);
             tmem_wait_ld();
             const int keys = p.len - (t0 + t) * kTile;
             if (keys < kTile) {
@@ -314,45 +363,35 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
                 for (int i = 0; i < kTile; ++i)
                     if (i >= keys) s[i] = 0xFF800000u;           // -inf
             }
-            float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            // Weights with the reference as it stands, and the tile's maximum beside them: only where some row's
+            // maximum passes the limit (and on the first tile, which has no reference yet) is the
+            // reference raised, and the weights are computed once more.
+            if (done == 0) {
+                const float top = row_max(s) * scale;
+                if (top > m) m = top;
+            }
+            float sum = row_weights(s, scale, m, t_s);
+            if (done > 0) {
+                const float top = row_max(s) * scale;
+                const bool raise = top > m + kRescaleAbove;
+                if (__any_sync(0xFFFFFFFFu, raise)) {
+                    const float before = m;
+                    if (raise) m = top;
+                    const float f = raise ? fast_exp2(before - m) : 1.f;
+                    l *= f;
 #pragma unroll
-            for (int i = 0; i < kTile; i += 4)
+                    for (int c = 0; c < D / 16; ++c) {
+                        uint32_t o[16];
+                        tmem_ld_row16(t_o + 16u * c, o);
+                        tmem_wait_ld();
 #pragma unroll
-                for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], __uint_as_float(s[i + k]));
-            const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
-            // raise the reference: the first tile's maximum, later only past 2^8 times the reference
-            const bool raise = done == 0 ? top > m : top > m + kRescaleAbove;
-            const float before = m;
-            if (raise) m = top;
-            if (done > 0 && __any_sync(0xFFFFFFFFu, raise)) {
-                const float f = raise ? fast_exp2(before - m) : 1.f;
-                l *= f;
-#pragma unroll
-                for (int c = 0; c < D / 32; ++c) {
-                    uint32_t o[32];
-                    tmem_ld_row32(t_o + 32u * c, o);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                    tmem_st_row32(t_o + 32u * c, o);
+                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                        tmem_st_row16(t_o + 16u * c, o);
+                    }
+                    sum = row_weights(s, scale, m, t_s);
                 }
             }
-            const float ref = m == -INFINITY ? 0.f : m;          // every score so far is -inf: weights 0, not NaN
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t pk[16];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float a = fast_exp2(fmaf(__uint_as_float(s[32 * c + 2 * i]), scale, -ref));
-                    const float b = fast_exp2(fmaf(__uint_as_float(s[32 * c + 2 * i + 1]), scale, -ref));
-                    sum[(2 * i) & 3] += a;
-                    sum[(2 * i + 1) & 3] += b;
-                    pk[i] = pack_bf16(a, b);
-                }
-                tmem_st_row16(t_s + 16u * c, pk);
-            }
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            l += sum;
             tmem_wait_st();
             tc_fence_before();
             mbar_arrive(bar(kBarP + L));
@@ -361,11 +400,19 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
         const int part = in_turn ? 2 * blockIdx.z + L : blockIdx.z;
         const int64_t at = static_cast<int64_t>(part) * p.n * p.q_heads + (g_row < rows ? out_row(g_row) : 0);
         const bool mine = active && g_row < rows;
-        if (done > 0 && ok) {
-            ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(kBarO + L), 0, abort_flag, p.status, limit));
-            tc_fence_after();
-        }
-        if (ok) {
+        if (done > 0 && ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(kBarO + L), 0, abort_flag, p.status, limit));
+        // Products are complete in the order of their issue.  Lane 0's O is complete: so are all products
+        // that read queries.  Lane 1's: so are all products of the block, unless the lanes take tiles in turn
+        // and lane 0 has the last one.
+        if (in_turn && L == 1 && ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(kBarO), 0, abort_flag, p.status, limit));
+        tc_fence_after();
+        if (ok && active) {
+            // O by rows from tensor memory into shared memory (a warp's 32 rows, 16-byte chunks in an order that
+            // spreads them over the banks), then whole rows to global memory.  Lane 0's rows lie on the
+            // queries, lane 1's on the first two stages: nothing reads them any more (see the waits above).
+            constexpr int CH = D / 4;                // 16-byte chunks of a row of fp32
+            static_assert(kM * D * 4 == 2 * Cfg::kTileBytes, "a lane's result takes the place of two tiles");
+            uint8_t* st = smem + (L * kM + (warp & 3) * 32) * D * 4;
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {
                 uint32_t o[32];
@@ -376,11 +423,18 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
 #pragma unroll
                     for (int i = 0; i < 32; ++i) o[i] = 0u;
                 }
-                if (mine) {
-                    uint4* dst = reinterpret_cast<uint4*>(p.part_o + at * D + 32 * c);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) dst[i] = make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-                }
+                for (int i = 0; i < 8; ++i)
+                    *reinterpret_cast<uint4*>(st + (lane * CH + ((c * 8 + i) ^ (lane & 7))) * 16) =
+                        make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+            }
+            __syncwarp();
+            const int64_t part0 = static_cast<int64_t>(part) * p.n * p.q_heads;
+            const int w0 = r0 + (in_turn ? 0 : L * kM) + (warp & 3) * 32, sub = lane / CH;
+            for (int r = sub; r < 32 && w0 + r < rows; r += 32 / CH) {
+                const int ch = lane % CH;
+                const uint4 v = *reinterpret_cast<const uint4*>(st + (r * CH + (ch ^ (r & 7))) * 16);
+                reinterpret_cast<uint4*>(p.part_o)[(part0 + out_row(w0 + r)) * CH + ch] = v;
             }
             if (mine) *reinterpret_cast<float2*>(p.part_ml + 2 * at) = make_float2(m, l);
         }
