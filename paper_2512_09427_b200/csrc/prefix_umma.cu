@@ -11,9 +11,10 @@
 // every K and V tile twice; otherwise both hold the same rows and take the tiles in turn, each with
 // a partial result of its own.
 //
-// Warps 0-3 and 4-7: softmax of lane 0 and 1, a thread per row (a row's 128 scores are one tcgen05.ld
-// per 32 columns: no shuffles); warp 8: TMA producer; warp 9: issues all products, in the order
-// PV0(j) QK0(j+1) PV1(j) QK1(j+1), so S of a lane is only overwritten by a product issued after the
+// Warps 0-7 and 8-15: softmax of lane 0 and 1, two threads per row, 64 keys each (no shuffles; with one
+// thread per row a scheduler has one warp of the lane and waits out every instruction's latency:
+// 4,200 cycles per pair of tiles against PAIR_CYCLES); warp 16: TMA producer; warp 17: issues all products, in the
+// order PV0(j) QK0(j+1) PV1(j) QK1(j+1), so S of a lane is only overwritten by a product issued after the
 // one that reads its P, and a full S tells that the lane's O is complete up to the tile before.
 //
 // The softmax keeps a reference m per row, raised only when a tile's maximum passes it by 2^8: P stays
@@ -30,8 +31,10 @@ using namespace dev;
 
 constexpr int kTile = kPrefixTile;                  // keys per tile
 constexpr int kM = 128;                             // rows per lane
-constexpr int kThreads = 320;
-constexpr int kProducerWarp = 8, kMmaWarp = 9;
+constexpr int kSoftmaxWarps = 16;                   // four warpgroups: lane 0 and 1, left and right 64 keys
+constexpr int kThreads = (kSoftmaxWarps + 2) * 32;
+constexpr int kProducerWarp = kSoftmaxWarps, kMmaWarp = kSoftmaxWarps + 1;
+constexpr int kLaneThreads = kSoftmaxWarps * 16;    // softmax threads of a lane
 constexpr int kMaxStages = 8;
 constexpr float kRescaleAbove = 8.f;
 constexpr int kHalfBytes = kTile * 128;             // 64 elements of 128 rows
@@ -44,7 +47,7 @@ struct Config {
     static constexpr int kHalves = D / 64;
     static constexpr int kTileBytes = kHalves * kHalfBytes;      // of K, of V, and of a lane's Q
     static constexpr int kStages = D == 128 ? 5 : 8;
-    static constexpr int kSmem = (2 + kStages) * kTileBytes + kNumBars * 8 + 64 + 1024;
+    static constexpr int kSmem = (2 + kStages) * kTileBytes + 2 * kM * 4 + kNumBars * 8 + 64 + 1024;
 };
 
 // D[tmem] (+)= A[tmem] . B[smem]
@@ -56,18 +59,7 @@ __device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64
         : "memory");
 }
 
-// 32 columns of the thread's own row (tensor-memory lane = 32 * (warp mod 4) + lane).
-__device__ __forceinline__ void tmem_ld_row32(uint32_t addr, uint32_t* r) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(addr)
-        : "memory");
-}
+// 16 columns of the thread's own row (tensor-memory lane = 32 * (warp mod 4) + lane); stores of 16 and of 8.
 __device__ __forceinline__ void tmem_ld_row16(uint32_t addr, uint32_t* r) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
@@ -82,6 +74,12 @@ __device__ __forceinline__ void tmem_st_row16(uint32_t addr, const uint32_t* r) 
         "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
         "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
+}
+
+__device__ __forceinline__ void tmem_st_row8(uint32_t addr, const uint32_t* r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"r"(addr), "r"(r[0]), "r"(r[1]),
+                 "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
 }
 
 // Two fp32 operations in one instruction.
@@ -102,33 +100,50 @@ __device__ __forceinline__ float2 add2(const float2& a, const float2& b) {
     return d;
 }
 
-__device__ __forceinline__ float row_max(const uint32_t (&s)[kTile]) {
+constexpr int kCols = kTile / 2;                    // scores per softmax thread
+
+__device__ __forceinline__ float row_max(const uint32_t (&s)[kCols]) {
     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-    for (int i = 0; i < kTile; i += 8)
+    for (int i = 0; i < kCols; i += 8)
 #pragma unroll
         for (int k = 0; k < 4; ++k) mx[k] = fmaxf(fmaxf(mx[k], __uint_as_float(s[i + 2 * k])), __uint_as_float(s[i + 2 * k + 1]));
     return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
 }
 
-// The row's weights 2^(s * scale - m), rounded to bf16, to tensor memory; their sum (unrounded).
-__device__ __forceinline__ float row_weights(const uint32_t (&s)[kTile], float scale, float m, uint32_t t_p) {
+// The thread's weights 2^(s * scale - m), rounded to bf16, to tensor memory; their sum (unrounded).
+__device__ __forceinline__ float row_weights(const uint32_t (&s)[kCols], float scale, float m, uint32_t t_p) {
     const float ref = m == -INFINITY ? 0.f : m;     // every score so far is -inf: weights 0, not NaN
     const float2 sc = make_float2(scale, scale), neg = make_float2(-ref, -ref);
     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        uint32_t pk[16];
+    for (int c = 0; c < kCols / 16; ++c) {
+        uint32_t pk[8];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            float2 x = fma2(make_float2(__uint_as_float(s[32 * c + 2 * i]), __uint_as_float(s[32 * c + 2 * i + 1])), sc, neg);
+        for (int i = 0; i < 8; ++i) {
+            float2 x = fma2(make_float2(__uint_as_float(s[16 * c + 2 * i]), __uint_as_float(s[16 * c + 2 * i + 1])), sc, neg);
             x = make_float2(fast_exp2(x.x), fast_exp2(x.y));
             sum[i & 1] = add2(sum[i & 1], x);
             pk[i] = pack_bf16(x.x, x.y);
         }
-        tmem_st_row16(t_p + 16u * c, pk);
+        tmem_st_row8(t_p + 8u * c, pk);
     }
     return (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
+}
+
+// Barrier over `threads` threads; the second form tells whether any of them says yes.  Every thread of a lane
+// comes to every one of its barriers, also after a wait has given up.
+__device__ __forceinline__ void lane_sync(int id, int threads) {
+    asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+__device__ __forceinline__ bool lane_any(int id, int threads, bool yes) {
+    uint32_t any;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, %3, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
+        : "=r"(any)
+        : "r"(static_cast<uint32_t>(yes)), "r"(id), "r"(threads)
+        : "memory");
+    return any != 0;
 }
 
 template <int D>
@@ -141,7 +156,8 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
     uint8_t* qbuf = smem;
     uint8_t* kv = qbuf + 2 * Cfg::kTileBytes;
-    uint64_t* bars = reinterpret_cast<uint64_t*>(kv + STAGES * Cfg::kTileBytes);
+    float* xch = reinterpret_cast<float*>(kv + STAGES * Cfg::kTileBytes);    // [lane][row], between a row's two threads
+    uint64_t* bars = reinterpret_cast<uint64_t*>(xch + 2 * kM);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + kNumBars);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(const_cast<int*>(abort_flag) + 1);
     const uint32_t bar0 = smem_u32(bars);
@@ -162,8 +178,8 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
     const int ahead = in_turn ? 2 : 1;               // K tiles requested before the first V tile
 
     if (tid < kNumBars) {
-        const bool many = (tid >= kBarQ && tid < kBarS) || (tid >= kBarP && tid < kBarO);   // a lane's 128 threads
-        mbar_init(bar(tid), many ? 128u : 1u);
+        const bool many = (tid >= kBarQ && tid < kBarS) || (tid >= kBarP && tid < kBarO);   // a lane's threads
+        mbar_init(bar(tid), many ? static_cast<uint32_t>(kLaneThreads) : 1u);
     }
     if (tid == 0) {
         *abort_flag = 0;
@@ -318,26 +334,28 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
         mbar_wait_slow(bar(kBarDrain), 0, nullptr, p.status, limit / 4 + 1);
     } else {
         // ------------------------------------------------------------------ softmax
-        const int L = warp >> 2;
+        const int L = warp >> 3, side = (warp >> 2) & 1;     // lane; left or right 64 keys of a tile
         const int row = (warp & 3) * 32 + lane;      // of the lane's tile
         const int g_row = r0 + (in_turn ? 0 : L * kM) + row;
+        const int sync_id = 1 + L;
         auto out_row = [&](int r) { return static_cast<int64_t>(r / p.group) * p.q_heads + head * p.group + r % p.group; };
         if (L == 0 || (lane1 && !in_turn)) {
             // queries to shared memory in the swizzled order; rows behind the last are zero
             constexpr int CH = D / 8;                // 16-byte chunks per row
+            constexpr int RSTEP = kLaneThreads / CH;
             const uint4* q = static_cast<const uint4*>(p.q);
             uint8_t* dst = qbuf + L * Cfg::kTileBytes;
-            uint4 v[CH];
-            const int c = tid % CH, rr = (tid & 127) / CH;       // chunk, first of the thread's rows
+            uint4 v[kM / RSTEP];
+            const int c = tid % CH, rr = (tid & (kLaneThreads - 1)) / CH;       // chunk, first of the thread's rows
 #pragma unroll
-            for (int i = 0; i < CH; ++i) {           // all loads before the first store
-                const int g = r0 + L * kM + rr + i * (128 / CH);
+            for (int i = 0; i < kM / RSTEP; ++i) {   // all loads before the first store
+                const int g = r0 + L * kM + rr + i * RSTEP;
                 v[i] = make_uint4(0u, 0u, 0u, 0u);
                 if (g < rows) v[i] = __ldg(q + out_row(g) * CH + c);
             }
 #pragma unroll
-            for (int i = 0; i < CH; ++i) {
-                const int r = rr + i * (128 / CH);
+            for (int i = 0; i < kM / RSTEP; ++i) {
+                const int r = rr + i * RSTEP;
                 *reinterpret_cast<uint4*>(dst + (c >> 3) * kHalfBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v[i];
             }
             fence_proxy_async();
@@ -345,98 +363,105 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
         }
         const uint32_t t_s = tmem + (static_cast<uint32_t>(warp & 3) << 21) + static_cast<uint32_t>(L) * 256u, t_o = t_s + 128u;
         const float scale = p.scale_log2;
-        float m = -INFINITY, l = 0.f;                // reference (log2 units) and sum
+        float m = -INFINITY, l = 0.f;                // reference (log2 units, the same in a row's two threads) and sum
         const int first_t = in_turn ? L : 0, step = in_turn ? 2 : 1;
         const bool active = L == 0 || lane1;
         uint32_t done = 0;                           // tiles of this lane so far
         for (int t = first_t; t < tiles && active; t += step, ++done) {
-            ok = __all_sync(0xFFFFFFFFu, mbar_wait_spin(bar(kBarS + L), done & 1u, abort_flag, p.status, limit));
-            if (!ok) break;
-            tc_fence_after();
-            uint32_t s[kTile];
+            if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait_spin(bar(kBarS + L), done & 1u, abort_flag, p.status, limit));
+            uint32_t s[kCols];
+            float top = -INFINITY;
+            if (ok) {
+                tc_fence_after();
 #pragma unroll
-            for (int c = 0; c < 8; ++c) tmem_ld_row16(t_s + 16u * c, s + 16 * c);
-            tmem_wait_ld();
-            const int keys = p.len - (t0 + t) * kTile;
-            if (keys < kTile) {
+                for (int c = 0; c < kCols / 16; ++c) tmem_ld_row16(t_s + static_cast<uint32_t>(side * kCols + 16 * c), s + 16 * c);
+                tmem_wait_ld();
+                const int keys = p.len - (t0 + t) * kTile - side * kCols;
+                if (keys < kCols) {
 #pragma unroll
-                for (int i = 0; i < kTile; ++i)
-                    if (i >= keys) s[i] = 0xFF800000u;           // -inf
+                    for (int i = 0; i < kCols; ++i)
+                        if (i >= keys) s[i] = 0xFF800000u;       // -inf
+                }
+                top = row_max(s) * scale;
             }
-            // Weights with the reference as it stands, and the tile's maximum beside them: only where some row's
-            // maximum passes the limit (and on the first tile, which has no reference yet) is the
-            // reference raised, and the weights are computed once more.
-            if (done == 0) {
-                const float top = row_max(s) * scale;
-                if (top > m) m = top;
-            }
-            float sum = row_weights(s, scale, m, t_s);
-            if (done > 0) {
-                const float top = row_max(s) * scale;
-                const bool raise = top > m + kRescaleAbove;
-                if (__any_sync(0xFFFFFFFFu, raise)) {
-                    const float before = m;
-                    if (raise) m = top;
+            // The barrier says whether some row of the lane has a maximum past its reference's limit (or no
+            // reference yet), and that all of S has been read: from here P may take its place.
+            if (lane_any(sync_id, kLaneThreads, done == 0 || top > m + kRescaleAbove)) {
+                float* x = xch + L * kM + row;
+                if (side == 0) *x = top;
+                lane_sync(sync_id, kLaneThreads);
+                if (side == 1) *x = top = fmaxf(*x, top);
+                lane_sync(sync_id, kLaneThreads);
+                if (side == 0) top = *x;
+                const bool raise = done == 0 ? top > m : top > m + kRescaleAbove;
+                const float before = m;
+                if (raise) m = top;
+                if (ok && done > 0) {                // the row's O, complete up to the tile before, to the new reference
                     const float f = raise ? fast_exp2(before - m) : 1.f;
                     l *= f;
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) {
+                    for (int c = 0; c < D / 32; ++c) {
                         uint32_t o[16];
-                        tmem_ld_row16(t_o + 16u * c, o);
+                        const uint32_t at = t_o + static_cast<uint32_t>(side * (D / 2) + 16 * c);
+                        tmem_ld_row16(at, o);
                         tmem_wait_ld();
 #pragma unroll
                         for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-                        tmem_st_row16(t_o + 16u * c, o);
+                        tmem_st_row16(at, o);
                     }
-                    sum = row_weights(s, scale, m, t_s);
                 }
             }
-            l += sum;
-            tmem_wait_st();
-            tc_fence_before();
-            mbar_arrive(bar(kBarP + L));
+            if (ok) {
+                l += row_weights(s, scale, m, t_s + static_cast<uint32_t>(side * kCols / 2));
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(bar(kBarP + L));
+            }
         }
         // the lane's result
-        const int part = in_turn ? 2 * blockIdx.z + L : blockIdx.z;
-        const int64_t at = static_cast<int64_t>(part) * p.n * p.q_heads + (g_row < rows ? out_row(g_row) : 0);
-        const bool mine = active && g_row < rows;
         if (done > 0 && ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(kBarO + L), 0, abort_flag, p.status, limit));
         // Products are complete in the order of their issue.  Lane 0's O is complete: so are all products
         // that read queries.  Lane 1's: so are all products of the block, unless the lanes take tiles in turn
         // and lane 0 has the last one.
         if (in_turn && L == 1 && ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(kBarO), 0, abort_flag, p.status, limit));
         tc_fence_after();
-        if (ok && active) {
-            // O by rows from tensor memory into shared memory (a warp's 32 rows, 16-byte chunks in an order that
-            // spreads them over the banks), then whole rows to global memory.  Lane 0's rows lie on the
-            // queries, lane 1's on the first two stages: nothing reads them any more (see the waits above).
+        if (active) {
+            // O by rows from tensor memory into shared memory (16-byte chunks in an order that spreads them over
+            // the banks), then whole rows to global memory.  Lane 0's rows lie on the queries, lane 1's on
+            // the first two stages: nothing reads them any more (see the waits above).
             constexpr int CH = D / 4;                // 16-byte chunks of a row of fp32
             static_assert(kM * D * 4 == 2 * Cfg::kTileBytes, "a lane's result takes the place of two tiles");
             uint8_t* st = smem + (L * kM + (warp & 3) * 32) * D * 4;
+            if (side == 1) xch[L * kM + row] = l;
+            if (ok) {
 #pragma unroll
-            for (int c = 0; c < D / 32; ++c) {
-                uint32_t o[32];
-                if (done > 0) {
-                    tmem_ld_row32(t_o + 32u * c, o);
-                    tmem_wait_ld();
-                } else {
+                for (int c = 0; c < D / 32; ++c) {
+                    uint32_t o[16];
+                    if (done > 0) {
+                        tmem_ld_row16(t_o + static_cast<uint32_t>(side * (D / 2) + 16 * c), o);
+                        tmem_wait_ld();
+                    } else {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) o[i] = 0u;
+                        for (int i = 0; i < 16; ++i) o[i] = 0u;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        *reinterpret_cast<uint4*>(st + (lane * CH + ((side * (CH / 2) + c * 4 + i) ^ (lane & 7))) * 16) =
+                            make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                 }
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    *reinterpret_cast<uint4*>(st + (lane * CH + ((c * 8 + i) ^ (lane & 7))) * 16) =
-                        make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
             }
-            __syncwarp();
-            const int64_t part0 = static_cast<int64_t>(part) * p.n * p.q_heads;
-            const int w0 = r0 + (in_turn ? 0 : L * kM) + (warp & 3) * 32, sub = lane / CH;
-            for (int r = sub; r < 32 && w0 + r < rows; r += 32 / CH) {
-                const int ch = lane % CH;
-                const uint4 v = *reinterpret_cast<const uint4*>(st + (r * CH + (ch ^ (r & 7))) * 16);
-                reinterpret_cast<uint4*>(p.part_o)[(part0 + out_row(w0 + r)) * CH + ch] = v;
+            lane_sync(sync_id, kLaneThreads);
+            if (ok) {
+                const int part = in_turn ? 2 * blockIdx.z + L : blockIdx.z;
+                const int64_t part0 = static_cast<int64_t>(part) * p.n * p.q_heads;
+                const int w0 = r0 + (in_turn ? 0 : L * kM) + (warp & 3) * 32, ch = lane % CH;
+                for (int r = side * 16 + lane / CH; r < side * 16 + 16 && w0 + r < rows; r += 32 / CH) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(st + (r * CH + (ch ^ (r & 7))) * 16);
+                    reinterpret_cast<uint4*>(p.part_o)[(part0 + out_row(w0 + r)) * CH + ch] = v;
+                }
+                if (side == 0 && g_row < rows)
+                    *reinterpret_cast<float2*>(p.part_ml + 2 * (part0 + out_row(g_row))) = make_float2(m, l + xch[L * kM + row]);
             }
-            if (mine) *reinterpret_cast<float2*>(p.part_ml + 2 * at) = make_float2(m, l);
         }
     }
     // ---- tear-down: every role comes here, on every path, and tensor memory is given back
