@@ -911,7 +911,7 @@ constexpr int64_t kLateTokensPerItem = 128;  // tokens per item on average, at m
 
 cudaError_t launch_tensor_decode(const odma_pool* pool, const TensorMaps& maps, const DecodeParams& p, int mode,
                                  const odma_tables* t, cudaStream_t stream, const InlineLens* lens, bool umma,
-                                 const SpanParams* span = nullptr) {
+                                 const SpanParams* span = nullptr, bool plan_complete = false) {
     const int n_ctas = t->n_ctas;
     const int32_t want = pool->alloc.config().readout;
     bool defer = want == ODMA_READOUT_LATE;
@@ -920,7 +920,8 @@ cudaError_t launch_tensor_decode(const odma_pool* pool, const TensorMaps& maps, 
                 t->kv_tokens * pool->kv_heads <= kLateTokensPerItem * t->n_items;
     defer = defer && mode == kModeSlab && !p.kv_fp8;
     // the kernels read their plan before they wait for the kernel ahead, which may be the one that writes it
-    const bool overlap = !built_on_device(t);
+    // (plan_complete: it is not)
+    const bool overlap = plan_complete || !built_on_device(t);
     return umma ? launch_decode_umma(maps, p, mode, n_ctas, stream, lens, span, defer, overlap)
                 : launch_decode_tc(maps, p, mode, n_ctas, stream, lens, overlap);
 }
@@ -1130,7 +1131,7 @@ int32_t odma_decode_attention_prefix(odma_pool* pool, int32_t layer, const void*
             if (make_tensor_maps(workspace, 2ll * pool->kv_heads * w.pad, D, 2, &ws_maps) != ODMA_OK) return ODMA_ERR_CUDA;
         }
         const TensorMaps& maps = pool->dtype == ODMA_DTYPE_FP8_E4M3 ? ws_maps : pool->maps;
-        const cudaError_t e = tensor ? launch_prefix_umma(maps.box[3], pp, s) : launch_prefix(pp, fp32, s);
+        const cudaError_t e = tensor ? launch_prefix_umma(maps.box[3], pp, pool->dtype == ODMA_DTYPE_FP8_E4M3, s) : launch_prefix(pp, fp32, s);
         if (e != cudaSuccess) return ODMA_ERR_CUDA;
     }
     {
@@ -1138,7 +1139,14 @@ int32_t odma_decode_attention_prefix(odma_pool* pool, int32_t layer, const void*
         cudaError_t e;
         if (uses_tc(pool, q_heads)) {
             if (p.stages < 2) return ODMA_ERR_INVALID;
-            e = launch_tensor_decode(pool, pool->maps, p, kModeSlab, tables, s, nullptr, uses_umma(pool, p.group, false));
+            // Behind the prefix's kernel the launch need not wait: the tables, queries and slab rows were complete before
+            // that kernel began (it waits for all work ahead of it), and it writes only the workspace.  So the tcgen05
+            // kernel runs as a chained launch, or the other one asks for its first rows early.
+            const bool behind = splits > 0 && tensor;
+            const bool umma = uses_umma(pool, p.group, behind);
+            p.chained = umma && behind ? 1 : 0;
+            p.early_ok = behind ? 1 : 0;
+            e = launch_tensor_decode(pool, pool->maps, p, kModeSlab, tables, s, nullptr, umma, nullptr, behind);
         } else {
             e = launch_decode_generic(p, pool->dtype, tables->n_ctas, s);
         }

@@ -209,7 +209,9 @@ struct PrefixSplit {
 };
 PrefixSplit prefix_split(int32_t rows, int32_t q_rows, int32_t kv_heads, int32_t len, int32_t sms, bool tensor);
 cudaError_t launch_prefix(const PrefixParams& p, bool fp32, cudaStream_t stream);
-cudaError_t launch_prefix_umma(const CUtensorMap& map, const PrefixParams& p, cudaStream_t stream);
+// `behind_dequant`: the kernel ahead is launch_dequant_prefix, itself launched behind everything else; otherwise this one
+// waits for all work ahead of it.  Either way the kernel behind it may begin at once (programmatic launch).
+cudaError_t launch_prefix_umma(const CUtensorMap& map, const PrefixParams& p, bool behind_dequant, cudaStream_t stream);
 cudaError_t launch_dequant_prefix(const void* k, const void* v, int64_t head_rows, int32_t len, int32_t pad,
                                   int32_t kv_heads, int32_t head_dim, void* out, cudaStream_t stream);
 cudaError_t launch_merge_prefix(const MergePrefixParams& p, bool fp32, cudaStream_t stream);

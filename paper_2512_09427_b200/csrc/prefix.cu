@@ -291,24 +291,22 @@ cudaError_t launch_generic_t(const PrefixParams& p, cudaStream_t s) {
 
 }  // namespace
 
-// Blocks along the prefix's keys: the number that minimises (waves of blocks) x (a block's time) + (the
-// merge's time), in sixteenths of what a block of the tensor-core kernel spends on one tile of 128 keys
-// and 128 rows.  A block costs kBlockUnits tiles more than its own (tensor-memory and barrier set-up,
-// queries, hand-over); every partial result costs its row a write and a read.
+// Blocks along the prefix's keys: the number that minimises (waves of blocks) x (a block's time) + (what the
+// partial results cost), by measured figures in ns.  Tensor cores (one block per SM): 6,500 for a block's set-up,
+// queries and hand-over, and per step of 64 keys 1,100 with two row tiles, 900 with one, 600 when one row
+// tile's steps go to the two lanes in turn.  Plain ALUs (8 rows, four blocks per SM): 3,000 and 5,000 per tile
+// of 128 keys.  A row's partial result costs its write and its read in the merge, 0.2.
 PrefixSplit prefix_split(int32_t rows, int32_t q_rows, int32_t kv_heads, int32_t len, int32_t sms, bool tensor) {
-    constexpr int64_t kBlockUnits = 6;
     const int64_t tiles = (len + kPrefixTile - 1) / kPrefixTile;
-    // tensor cores: one block per SM, two tiles of 128 rows; plain ALUs: 8 rows, several blocks per SM
     const int64_t blocks = kv_heads * static_cast<int64_t>(tensor ? (rows + 255) / 256 : (rows + kRows - 1) / kRows);
     const int64_t room = tensor ? sms : 4ll * sms;
     PrefixSplit best{1, 0};
     int64_t least = INT64_MAX;
     for (int32_t s = 1; s <= std::min<int64_t>(tiles, kMaxPrefixSplits); ++s) {
         const int64_t waves = (blocks * s + room - 1) / room, each = (tiles + s - 1) / s;
-        for (int32_t turn = 0; turn <= (tensor && rows <= 128 && tiles >= 2 * s ? 1 : 0); ++turn) {
-            // one row tile alone waits for itself (its softmax and its products in turn): twice a tile's time
-            const int64_t work = !tensor ? 4 * each : turn ? each : 2 * each, parts = turn ? 2 * s : s;
-            const int64_t cost = 16 * waves * (work + kBlockUnits) + parts * (2 + q_rows / 128);
+        for (int32_t turn = 0; turn <= (tensor && rows <= 128 ? 1 : 0); ++turn) {
+            const int64_t block = !tensor ? 3000 + 5000 * each : 6500 + 2 * each * (turn ? 600 : rows <= 128 ? 900 : 1100);
+            const int64_t parts = turn ? 2 * s : s, cost = waves * block + parts * q_rows / 5;
             if (cost < least) {
                 least = cost;
                 best = PrefixSplit{static_cast<int32_t>(parts), turn};

@@ -174,6 +174,9 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
     auto bar = [&](int i) { return bar0 + 8u * static_cast<uint32_t>(i); };
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int64_t limit = p.wait_limit_ns;
+    // The kernel behind this one (the requests' own parts) reads nothing that this one or the one ahead of it writes: its
+    // blocks may begin on every SM that this one leaves idle or is done with.
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     // the block's work
     const int head = blockIdx.y;
@@ -212,6 +215,7 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
         // ------------------------------------------------------------------ producer
         // Ring order: K of the first `ahead` steps, then V(u), K(u + ahead) for each step u.
         if (lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map)) : "memory");
+        asm volatile("griddepcontrol.wait;" ::: "memory");           // 8-bit pools: the kernel ahead writes these rows
         uint32_t issued = 0;
         auto load = [&](bool is_v, int u) {
             const uint32_t stage = issued % STAGES, use = issued / STAGES;
@@ -491,7 +495,7 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
 }
 
 template <int D>
-cudaError_t launch_t(const CUtensorMap& map, const PrefixParams& p, cudaStream_t stream) {
+cudaError_t launch_t(const CUtensorMap& map, const PrefixParams& p, bool behind_dequant, cudaStream_t stream) {
     static bool configured[64] = {false};             // the opt-in to large shared memory is per device
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -505,15 +509,24 @@ cudaError_t launch_t(const CUtensorMap& map, const PrefixParams& p, cudaStream_t
     const int rows = p.n * p.group;
     const dim3 grid(static_cast<unsigned>((rows + 2 * kM - 1) / (2 * kM)), static_cast<unsigned>(p.kv_heads),
                     static_cast<unsigned>(p.in_turn ? p.splits / 2 : p.splits));
-    prefix_umma_kernel<D><<<grid, kThreads, Config<D>::kSmem, stream>>>(map, p);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = Config<D>::kSmem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = behind_dequant ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, prefix_umma_kernel<D>, map, p);
 }
 
 }  // namespace
 
-cudaError_t launch_prefix_umma(const CUtensorMap& map, const PrefixParams& p, cudaStream_t stream) {
+cudaError_t launch_prefix_umma(const CUtensorMap& map, const PrefixParams& p, bool behind_dequant, cudaStream_t stream) {
     if (p.splits < 1 || p.len < 1) return cudaSuccess;
-    return p.head_dim == 128 ? launch_t<128>(map, p, stream) : launch_t<64>(map, p, stream);
+    return p.head_dim == 128 ? launch_t<128>(map, p, behind_dequant, stream) : launch_t<64>(map, p, behind_dequant, stream);
 }
 
 }  // namespace odma
