@@ -191,44 +191,61 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
     const int turn = in_turn ? 2 : 1, ahead = 2 * turn;         // K of a step is asked for `ahead` steps before its V
     auto lane_steps = [&](int L) { return in_turn ? (steps - L + 1) / 2 : steps; };
 
-    if (tid < kNumBars) {
-        const bool softmax = tid >= kBarQ && tid < kBarS;                        // arrivals of a lane's softmax warps
-        const bool shared = tid >= kBarEmpty && tid < kBarQ && lane1;            // both lanes hand every tile back
-        mbar_init(bar(tid), softmax ? kLaneThreads / 32u : shared ? 2u : 1u);
-    }
-    if (tid == 0) {
-        *abort_flag = 0;
+    const uint32_t kv_u32 = smem_u32(kv), q_u32 = smem_u32(qbuf);
+    bool ok = true;
+    auto out_row = [&](int r) { return (r / p.group) * p.q_heads + head * p.group + r % p.group; };    // row of q and of a partial result
+
+    // ---- set-up, the roles side by side: barriers and the first loads; tensor memory; the queries' loads
+    uint32_t issued = 0;
+    auto load = [&](bool is_v, int u) {              // the producer's next stage
+        const uint32_t stage = issued % STAGES, use = issued / STAGES;
+        ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(kBarEmpty + stage), (use & 1u) ^ 1u, abort_flag, p.status, limit));
+        if (!ok) return;
+        if (lane == 0) mbar_expect_tx(bar(kBarFull + stage), static_cast<uint32_t>(Cfg::kStageBytes));
+        __syncwarp();
+        if (lane < Cfg::kHalves)                     // a box of 64 rows per 128-byte column block
+            tma_load_2d(kv_u32 + stage * Cfg::kStageBytes + lane * kHalfBytes, &map, lane * 64,
+                        static_cast<int32_t>((is_v ? p.v_row0 : p.k_row0) + head * p.head_rows + k0 + u * kStep), bar(kBarFull + stage));
+        ++issued;
+    };
+    constexpr int QCH = D / 8;                       // 16-byte chunks of a query row
+    constexpr int QLOADS = kM * QCH / kLaneThreads;  // per thread of a lane
+    constexpr int QROWS = 32 / QCH;                  // rows per warp and load
+    uint4 qv[QLOADS];
+    if (warp == kProducerWarp) {
+        for (int i = lane; i < kNumBars; i += 32) {
+            const bool softmax = i >= kBarQ && i < kBarS;                        // arrivals of a lane's softmax warps
+            const bool shared = i >= kBarEmpty && i < kBarQ && lane1;            // both lanes hand every stage back
+            mbar_init(bar(i), softmax ? kLaneThreads / 32u : shared ? 2u : 1u);
+        }
+        if (lane == 0) *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-    }
-    if (warp == kMmaWarp) {
+        __syncwarp();
+        asm volatile("griddepcontrol.wait;" ::: "memory");                       // 8-bit pools: the kernel ahead writes these rows
+        for (int u = 0; u < min(ahead, steps) && ok; ++u) load(false, u);        // (as many stages as this are free)
+    } else if (warp == kMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u)
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    } else if (warp < kSoftmaxWarps) {
+        // a warp loads 16 of its lane's 128 rows, QROWS at a time; one thread works out one row's place
+        const int g0 = r0 + (in_turn ? 0 : (warp >> 3) * kM) + (warp & 7) * (QROWS * QLOADS);
+        const int mine = out_row(min(g0 + (lane & (QROWS * QLOADS - 1)), rows - 1));
+#pragma unroll
+        for (int i = 0; i < QLOADS; ++i) {
+            const int r = i * QROWS + lane / QCH, at = __shfl_sync(0xFFFFFFFFu, mine, r);
+            qv[i] = make_uint4(0u, 0u, 0u, 0u);      // rows behind the last are zero
+            if (g0 + r < rows) qv[i] = __ldg(static_cast<const uint4*>(p.q) + static_cast<int64_t>(at) * QCH + lane % QCH);
+        }
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
-    const uint32_t kv_u32 = smem_u32(kv), q_u32 = smem_u32(qbuf);
-    bool ok = true;
+
     if (warp == kProducerWarp) {
         // ------------------------------------------------------------------ producer
         // Ring order: K of the first `ahead` steps, then V(u), K(u + ahead) for each step u.
-        if (lane == 0) asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&map)) : "memory");
-        asm volatile("griddepcontrol.wait;" ::: "memory");           // 8-bit pools: the kernel ahead writes these rows
-        uint32_t issued = 0;
-        auto load = [&](bool is_v, int u) {
-            const uint32_t stage = issued % STAGES, use = issued / STAGES;
-            ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(kBarEmpty + stage), (use & 1u) ^ 1u, abort_flag, p.status, limit));
-            if (!ok) return;
-            if (lane == 0) mbar_expect_tx(bar(kBarFull + stage), static_cast<uint32_t>(Cfg::kStageBytes));
-            __syncwarp();
-            if (lane < Cfg::kHalves)                 // a box of 64 rows per 128-byte column block
-                tma_load_2d(kv_u32 + stage * Cfg::kStageBytes + lane * kHalfBytes, &map, lane * 64,
-                            static_cast<int32_t>((is_v ? p.v_row0 : p.k_row0) + head * p.head_rows + k0 + u * kStep), bar(kBarFull + stage));
-            ++issued;
-        };
-        for (int u = 0; u < min(ahead, steps) && ok; ++u) load(false, u);
         for (int u = 0; u < steps && ok; ++u) {
             load(true, u);
             if (ok && u + ahead < steps) load(false, u + ahead);
@@ -349,26 +366,13 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
         const int L = warp >> 3, side = (warp >> 2) & 1;     // lane; left or right 64 keys of a tile
         const int row = (warp & 3) * 32 + lane;      // of the lane's tile
         const int g_row = r0 + (in_turn ? 0 : L * kM) + row;
-        const int sync_id = 1 + L, pair_id = 3 + L * 4 + (warp & 3);     // barriers of the lane, and of the row's two warps
-        auto out_row = [&](int r) { return static_cast<int64_t>(r / p.group) * p.q_heads + head * p.group + r % p.group; };
-        if (L == 0 || (lane1 && !in_turn)) {
-            // queries to shared memory in the swizzled order; rows behind the last are zero
-            constexpr int CH = D / 8;                // 16-byte chunks per row
-            constexpr int RSTEP = kLaneThreads / CH;
-            const uint4* q = static_cast<const uint4*>(p.q);
+        const int pair_id = 1 + L * 4 + (warp & 3);  // barrier of the row's two warps
+        if (L == 0 || (lane1 && !in_turn)) {         // queries to shared memory, in the swizzled order
             uint8_t* dst = qbuf + L * Cfg::kQBytes;
-            uint4 v[kM / RSTEP];
-            const int c = tid % CH, rr = (tid & (kLaneThreads - 1)) / CH;       // chunk, first of the thread's rows
 #pragma unroll
-            for (int i = 0; i < kM / RSTEP; ++i) {   // all loads before the first store
-                const int g = r0 + L * kM + rr + i * RSTEP;
-                v[i] = make_uint4(0u, 0u, 0u, 0u);
-                if (g < rows) v[i] = __ldg(q + out_row(g) * CH + c);
-            }
-#pragma unroll
-            for (int i = 0; i < kM / RSTEP; ++i) {
-                const int r = rr + i * RSTEP;
-                *reinterpret_cast<uint4*>(dst + (c >> 3) * kQHalfBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v[i];
+            for (int i = 0; i < QLOADS; ++i) {
+                const int r = (warp & 7) * (QROWS * QLOADS) + i * QROWS + lane / QCH, c = lane % QCH;
+                *reinterpret_cast<uint4*>(dst + (c >> 3) * kQHalfBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = qv[i];
             }
             fence_proxy_async();
             __syncwarp();
@@ -446,12 +450,11 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
         if (ok && two) ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(kBarO + 1), 0, abort_flag, p.status, limit));
         tc_fence_after();
         if (active) {
-            // O by rows from tensor memory into shared memory (16-byte chunks in an order that spreads them over
-            // the banks), then whole rows to global memory.  Lane 0's rows lie on the queries, lane 1's on
-            // the first stages.
-            constexpr int CH = D / 4;                // 16-byte chunks of a row of fp32
-            static_assert(kM * D * 4 == 2 * Cfg::kQBytes && kM * D * 4 <= Cfg::kStages * Cfg::kStageBytes, "where a lane's result goes");
-            uint8_t* st = smem + (L * kM + (warp & 3) * 32) * D * 4;
+            // O by rows from tensor memory into shared memory (over queries and stages; a row's pitch is 16 bytes more than
+            // its size, which spreads 16-byte chunks over the banks), then a bulk copy per row to global memory.
+            constexpr uint32_t PITCH = D * 4 + 16;
+            static_assert(2 * kM * PITCH <= 2 * Cfg::kQBytes + Cfg::kStages * Cfg::kStageBytes, "where the results go");
+            const uint32_t st = static_cast<uint32_t>(L * kM + row) * PITCH;
             if (side == 1) xch[L * kM + row] = l;
             if (ok) {
 #pragma unroll
@@ -466,21 +469,20 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
                     }
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        *reinterpret_cast<uint4*>(st + (lane * CH + ((side * (CH / 2) + c * 4 + i) ^ (lane & 7))) * 16) =
+                        *reinterpret_cast<uint4*>(smem + st + (side * (D / 2) + 16 * c + 4 * i) * 4) =
                             make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
                 }
             }
-            lane_sync(sync_id, kLaneThreads);
-            if (ok) {
+            fence_proxy_async();
+            lane_sync(pair_id, 64);
+            if (ok && side == 0 && g_row < rows) {
                 const int part = in_turn ? 2 * blockIdx.z + L : blockIdx.z;
-                const int64_t part0 = static_cast<int64_t>(part) * p.n * p.q_heads;
-                const int w0 = r0 + (in_turn ? 0 : L * kM) + (warp & 3) * 32, ch = lane % CH;
-                for (int r = side * 16 + lane / CH; r < side * 16 + 16 && w0 + r < rows; r += 32 / CH) {
-                    const uint4 v = *reinterpret_cast<const uint4*>(st + (r * CH + (ch ^ (r & 7))) * 16);
-                    reinterpret_cast<uint4*>(p.part_o)[(part0 + out_row(w0 + r)) * CH + ch] = v;
-                }
-                if (side == 0 && g_row < rows)
-                    *reinterpret_cast<float2*>(p.part_ml + 2 * (part0 + out_row(g_row))) = make_float2(m, l + xch[L * kM + row]);
+                const int64_t at = static_cast<int64_t>(part) * p.n * p.q_heads + out_row(g_row);
+                asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(p.part_o + at * D), "r"(smem_u32(smem) + st), "r"(D * 4)
+                             : "memory");
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+                *reinterpret_cast<float2*>(p.part_ml + 2 * at) = make_float2(m, l + xch[L * kM + row]);
+                asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");        // written: the block may end
             }
         }
     }
