@@ -27,6 +27,7 @@ using namespace dev;
 constexpr int kRows = 8;            // query rows a block of the generic kernel carries
 constexpr int kWarps = 4;
 constexpr int kMergeWarps = 8;
+constexpr int kBatch = 8;            // parts of a row that are under way at a time in the merge
 
 __device__ __forceinline__ void unpack16(const uint4& v, float (&x)[4], float) {
     x[0] = __uint_as_float(v.x);
@@ -203,14 +204,61 @@ __global__ void __launch_bounds__(256) dequant_prefix_kernel(const uint8_t* k, c
 }
 
 // Blocks [0, n_items): the stream that begins with this item, a warp per query head.  Blocks behind
-// them: the requests, for those without a token of their own.  A row's parts are its own pieces and then
-// the prefix's splits, in that order.  32 at a time: a lane fetches one part's (m, l), the warp finds
-// the maximum and every part's factor 2^(m - M), and the rows are added up with all loads independent
-// of one another (folded one after the other, 15 parts took 13 us; a chain of L2 round trips).
+// them: the requests, for those without a token of their own.  A row's parts are the prefix's splits and
+// then its own pieces, in that order, up to 32 at a time: a lane fetches one part's (m, l), the warp finds
+// the maximum and every part's factor 2^(m - M), and the rows are added up, kBatch loads under way at a time
+// (folded one after the other, a chain of L2 round trips, 15 parts took 13 us).
+//
+// Launched programmatically: a block begins once every block of the kernel ahead (the requests' own parts)
+// has begun and knows the prefix's kernel complete.  So the plan and the prefix's parts, most of the
+// work, are read before the wait for that kernel's end, and only the own pieces after it.
+template <int V>
+struct MergeRow {
+    float M = -INFINITY, L = 0.f, acc[V];
+
+    // `count` parts: rows of D floats `o_stride` apart from `o` (the lane's own elements), (m, l) pairs
+    // `ml_stride` apart from `ml`; every row times `scale`.
+    __device__ __forceinline__ void add(const float* o, int64_t o_stride, const float* ml, int64_t ml_stride, int parts, float scale) {
+        const int lane = threadIdx.x & 31;
+        for (int s0 = 0; s0 < parts; s0 += 32) {
+            const int count = min(32, parts - s0);
+            float2 v = make_float2(-INFINITY, 0.f);
+            if (lane < count) v = __ldcg(reinterpret_cast<const float2*>(ml + (s0 + lane) * ml_stride));
+            float x[kBatch][V];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k)
+                if (k < count) load_row(o + (s0 + k) * o_stride, x[k]);
+            float top = fmaxf(M, v.x);
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
+            const float e = v.x == -INFINITY ? 0.f : fast_exp2(v.x - top), old = M == -INFINITY ? 0.f : fast_exp2(M - top);
+            float sum = v.y * e;
+#pragma unroll
+            for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
+            L = fmaf(L, old, sum);
+            M = top;
+#pragma unroll
+            for (int i = 0; i < V; ++i) acc[i] *= old;
+            const float f = e * scale;
+            for (int k0 = 0; k0 < count; k0 += kBatch) {
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k) {
+                    const float w = __shfl_sync(0xFFFFFFFFu, f, (k0 + k) & 31);
+                    if (k0 + k < count)
+#pragma unroll
+                        for (int i = 0; i < V; ++i) acc[i] = fmaf(x[k][i], w, acc[i]);
+                }
+#pragma unroll
+                for (int k = 0; k < kBatch; ++k)
+                    if (k0 + kBatch + k < count) load_row(o + (s0 + k0 + kBatch + k) * o_stride, x[k]);
+            }
+        }
+    }
+};
+
 template <typename T, int V>        // head_dim = 32 * V
 __global__ void __launch_bounds__(kMergeWarps * 32) merge_prefix_kernel(const MergePrefixParams p) {
     constexpr int D = 32 * V;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
     int req, head, heads = 1, slot0 = 0, pieces = 0;
     if (static_cast<int>(blockIdx.x) < p.n_items) {
         const int4 a = __ldg(p.items + 2 * blockIdx.x), b = __ldg(p.items + 2 * blockIdx.x + 1);
@@ -230,43 +278,17 @@ __global__ void __launch_bounds__(kMergeWarps * 32) merge_prefix_kernel(const Me
     for (int g = threadIdx.x >> 5; g < heads * p.group; g += kMergeWarps) {
         const int64_t row = static_cast<int64_t>(req) * p.q_heads + head * p.group + g;
         const int64_t own_row = static_cast<int64_t>(slot0) * p.group + g;
-        float M = -INFINITY, L = 0.f, acc[V];
+        MergeRow<V> r;
 #pragma unroll
-        for (int i = 0; i < V; ++i) acc[i] = 0.f;
-        const int parts = pieces + p.splits;
-        for (int s0 = 0; s0 < parts; s0 += 32) {
-            const int s = s0 + lane, count = min(32, parts - s0);
-            float2 ml = make_float2(-INFINITY, 0.f);
-            if (s < parts) ml = __ldcg(reinterpret_cast<const float2*>(s < pieces ? p.own_ml + 2 * (own_row + static_cast<int64_t>(s) * p.group)
-                                                                                  : p.part_ml + 2 * ((s - pieces) * split_rows + row)));
-            float top = fmaxf(M, ml.x);
+        for (int i = 0; i < V; ++i) r.acc[i] = 0.f;
+        r.add(p.part_o + row * D + lane * V, split_rows * D, p.part_ml + 2 * row, 2 * split_rows, p.splits, p.v_scale);
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        r.add(p.own_o + own_row * D + lane * V, static_cast<int64_t>(p.group) * D, p.own_ml + 2 * own_row, 2ll * p.group, pieces, 1.f);
+        const float inv = r.L > 0.f ? 1.f / r.L : (r.L == 0.f ? 0.f : r.L);      // no key at all: zeros
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
-            const float e = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - top), old = M == -INFINITY ? 0.f : fast_exp2(M - top);
-            float sum = ml.y * e;
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-            L = fmaf(L, old, sum);
-            M = top;
-#pragma unroll
-            for (int i = 0; i < V; ++i) acc[i] *= old;
-            const float f = s < pieces ? e : e * p.v_scale;
-#pragma unroll 8
-            for (int k = 0; k < count; ++k) {
-                const float w = __shfl_sync(0xFFFFFFFFu, f, k);
-                const float* src = s0 + k < pieces ? p.own_o + (own_row + static_cast<int64_t>(s0 + k) * p.group) * D
-                                                   : p.part_o + ((s0 + k - pieces) * split_rows + row) * D;
-                float x[V];
-                load_row(src + lane * V, x);
-#pragma unroll
-                for (int i = 0; i < V; ++i) acc[i] = fmaf(x[i], w, acc[i]);
-            }
-        }
-        const float inv = L > 0.f ? 1.f / L : (L == 0.f ? 0.f : L);      // no key at all: zeros
-#pragma unroll
-        for (int i = 0; i < V; ++i) acc[i] *= inv;
-        store_row(static_cast<T*>(p.out) + row * D + lane * V, acc);
-        if (lane == 0 && p.lse) p.lse[row] = L == 0.f ? -INFINITY : (M + log2f(L)) * 0.6931471805599453f;
+        for (int i = 0; i < V; ++i) r.acc[i] *= inv;
+        store_row(static_cast<T*>(p.out) + row * D + lane * V, r.acc);
+        if (lane == 0 && p.lse) p.lse[row] = r.L == 0.f ? -INFINITY : (r.M + log2f(r.L)) * 0.6931471805599453f;
     }
 }
 
