@@ -930,15 +930,22 @@ decode_generic_kernel(const DecodeParams p) {
                 for (int r = 0; r < GC; ++r) s[r] = 0.f;
                 if (valid) {
                     const uint4* kp = reinterpret_cast<const uint4*>(K + static_cast<int64_t>(j) * D);
-#pragma unroll 2
-                    for (int v = 0; v < D / VE; ++v) {
-                        float x[VE];
-                        Vec16<T>::unpack(kp[v], x);
+                    // up to eight vectors of the row are under way at a time: a few keys per warp are a chain of round trips
+                    constexpr int KB = D / VE < 8 ? D / VE : 8;
+                    for (int v0 = 0; v0 < D / VE; v0 += KB) {
+                        uint4 kv[KB];
 #pragma unroll
-                        for (int e = 0; e < VE; ++e)
+                        for (int v = 0; v < KB; ++v) kv[v] = kp[v0 + v];
 #pragma unroll
-                            for (int r = 0; r < GC; ++r)
-                                if (r < gc) s[r] = fmaf(q_s[r][v * VE + e], x[e], s[r]);
+                        for (int v = 0; v < KB; ++v) {
+                            float x[VE];
+                            Vec16<T>::unpack(kv[v], x);
+#pragma unroll
+                            for (int e = 0; e < VE; ++e)
+#pragma unroll
+                                for (int r = 0; r < GC; ++r)
+                                    if (r < gc) s[r] = fmaf(q_s[r][(v0 + v) * VE + e], x[e], s[r]);
+                        }
                     }
                 }
 #pragma unroll
@@ -963,17 +970,25 @@ decode_generic_kernel(const DecodeParams p) {
                 }
                 __syncwarp();
                 const int cnt = min(32, ntok - j0);
-                for (int jj = 0; jj < cnt; ++jj) {
-                    float v[DPL];
+                constexpr int VB = 8;               // value rows under way at a time
+                for (int b0 = 0; b0 < cnt; b0 += VB) {
+                    float v[VB][DPL];
 #pragma unroll
-                    for (int c = 0; c < DPL; ++c)
-                        v[c] = to_float(V[static_cast<int64_t>(j0 + jj) * D + lane + 32 * c]);
+                    for (int u = 0; u < VB; ++u)
+                        if (b0 + u < cnt)
 #pragma unroll
-                    for (int r = 0; r < GC; ++r) {
-                        if (r >= gc) continue;
-                        const float pr = p_s[warp][r][jj];
+                            for (int c = 0; c < DPL; ++c)
+                                v[u][c] = to_float(V[static_cast<int64_t>(j0 + b0 + u) * D + lane + 32 * c]);
 #pragma unroll
-                        for (int c = 0; c < DPL; ++c) o[r][c] = fmaf(pr, v[c], o[r][c]);
+                    for (int u = 0; u < VB; ++u) {
+                        if (b0 + u >= cnt) break;
+#pragma unroll
+                        for (int r = 0; r < GC; ++r) {
+                            if (r >= gc) continue;
+                            const float pr = p_s[warp][r][b0 + u];
+#pragma unroll
+                            for (int c = 0; c < DPL; ++c) o[r][c] = fmaf(pr, v[u][c], o[r][c]);
+                        }
                     }
                 }
                 __syncwarp();

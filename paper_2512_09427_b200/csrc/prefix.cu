@@ -108,14 +108,20 @@ __global__ void __launch_bounds__(kWarps * 32) prefix_generic_kernel(const Prefi
         for (int r = 0; r < kRows; ++r) s[r] = 0.f;
         if (valid) {
             const uint4* kp = reinterpret_cast<const uint4*>(K + static_cast<int64_t>(j0 + lane) * D);
-#pragma unroll 4
-            for (int v = 0; v < D / VE; ++v) {
-                float x[VE];
-                unpack16(__ldg(kp + v), x, T());
+            constexpr int KB = D / VE < 8 ? D / VE : 8;      // vectors of the row under way at a time
+            for (int v0 = 0; v0 < D / VE; v0 += KB) {
+                uint4 kv[KB];
 #pragma unroll
-                for (int e = 0; e < VE; ++e)
+                for (int v = 0; v < KB; ++v) kv[v] = __ldg(kp + v0 + v);
 #pragma unroll
-                    for (int r = 0; r < kRows; ++r) s[r] = fmaf(q_s[r][v * VE + e], x[e], s[r]);
+                for (int v = 0; v < KB; ++v) {
+                    float x[VE];
+                    unpack16(kv[v], x, T());
+#pragma unroll
+                    for (int e = 0; e < VE; ++e)
+#pragma unroll
+                        for (int r = 0; r < kRows; ++r) s[r] = fmaf(q_s[r][(v0 + v) * VE + e], x[e], s[r]);
+                }
             }
         }
 #pragma unroll
@@ -139,15 +145,23 @@ __global__ void __launch_bounds__(kWarps * 32) prefix_generic_kernel(const Prefi
         }
         __syncwarp();
         const int cnt = min(32, last - j0);
-        for (int jj = 0; jj < cnt; ++jj) {
-            float v[DPL];
+        constexpr int VB = 8;                        // value rows under way at a time
+        for (int b0 = 0; b0 < cnt; b0 += VB) {
+            float v[VB][DPL];
 #pragma unroll
-            for (int c = 0; c < DPL; ++c) v[c] = as_float(V[static_cast<int64_t>(j0 + jj) * D + lane + 32 * c]);
+            for (int u = 0; u < VB; ++u)
+                if (b0 + u < cnt)
 #pragma unroll
-            for (int r = 0; r < kRows; ++r) {
-                const float pr = p_s[warp][r][jj];
+                    for (int c = 0; c < DPL; ++c) v[u][c] = as_float(V[static_cast<int64_t>(j0 + b0 + u) * D + lane + 32 * c]);
 #pragma unroll
-                for (int c = 0; c < DPL; ++c) o[r][c] = fmaf(pr, v[c], o[r][c]);
+            for (int u = 0; u < VB; ++u) {
+                if (b0 + u >= cnt) break;
+#pragma unroll
+                for (int r = 0; r < kRows; ++r) {
+                    const float pr = p_s[warp][r][b0 + u];
+#pragma unroll
+                    for (int c = 0; c < DPL; ++c) o[r][c] = fmaf(pr, v[u][c], o[r][c]);
+                }
             }
         }
         __syncwarp();
