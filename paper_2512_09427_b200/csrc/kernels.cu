@@ -925,13 +925,26 @@ decode_generic_kernel(const DecodeParams p) {
             for (int j0 = warp * 32; j0 < ntok; j0 += kGenericWarps * 32) {
                 const int j = j0 + lane;
                 const bool valid = j < ntok;
+                // the first value rows are asked for before the scores need their keys
+                const int cnt = min(32, ntok - j0);
+                constexpr int VB = DPL > 2 ? 8 : 16;    // value rows under way at a time
+                float v[VB][DPL];
+                auto values = [&](int b0) {
+#pragma unroll
+                    for (int u = 0; u < VB; ++u)
+                        if (b0 + u < cnt)
+#pragma unroll
+                            for (int c = 0; c < DPL; ++c)
+                                v[u][c] = to_float(V[static_cast<int64_t>(j0 + b0 + u) * D + lane + 32 * c]);
+                };
+                values(0);
                 float s[GC];
 #pragma unroll
                 for (int r = 0; r < GC; ++r) s[r] = 0.f;
                 if (valid) {
                     const uint4* kp = reinterpret_cast<const uint4*>(K + static_cast<int64_t>(j) * D);
-                    // up to eight vectors of the row are under way at a time: a few keys per warp are a chain of round trips
-                    constexpr int KB = D / VE < 8 ? D / VE : 8;
+                    // up to sixteen vectors of the row are under way at a time: a few keys per warp are a chain of round trips
+                    constexpr int KB = D / VE < 16 ? D / VE : 16;
                     for (int v0 = 0; v0 < D / VE; v0 += KB) {
                         uint4 kv[KB];
 #pragma unroll
@@ -969,16 +982,7 @@ decode_generic_kernel(const DecodeParams p) {
                     p_s[warp][r][lane] = pr;
                 }
                 __syncwarp();
-                const int cnt = min(32, ntok - j0);
-                constexpr int VB = 8;               // value rows under way at a time
                 for (int b0 = 0; b0 < cnt; b0 += VB) {
-                    float v[VB][DPL];
-#pragma unroll
-                    for (int u = 0; u < VB; ++u)
-                        if (b0 + u < cnt)
-#pragma unroll
-                            for (int c = 0; c < DPL; ++c)
-                                v[u][c] = to_float(V[static_cast<int64_t>(j0 + b0 + u) * D + lane + 32 * c]);
 #pragma unroll
                     for (int u = 0; u < VB; ++u) {
                         if (b0 + u >= cnt) break;
@@ -990,6 +994,7 @@ decode_generic_kernel(const DecodeParams p) {
                             for (int c = 0; c < DPL; ++c) o[r][c] = fmaf(pr, v[u][c], o[r][c]);
                         }
                     }
+                    values(b0 + VB);
                 }
                 __syncwarp();
             }

@@ -103,12 +103,24 @@ __global__ void __launch_bounds__(kWarps * 32) prefix_generic_kernel(const Prefi
     }
     for (int j0 = first + warp * 32; j0 < last; j0 += kWarps * 32) {
         const bool valid = j0 + lane < last;
+        // the first value rows are asked for before the scores need their keys
+        const int cnt = min(32, last - j0);
+        constexpr int VB = DPL > 2 ? 8 : 16;         // value rows under way at a time
+        float v[VB][DPL];
+        auto values = [&](int b0) {
+#pragma unroll
+            for (int u = 0; u < VB; ++u)
+                if (b0 + u < cnt)
+#pragma unroll
+                    for (int c = 0; c < DPL; ++c) v[u][c] = as_float(V[static_cast<int64_t>(j0 + b0 + u) * D + lane + 32 * c]);
+        };
+        values(0);
         float s[kRows];
 #pragma unroll
         for (int r = 0; r < kRows; ++r) s[r] = 0.f;
         if (valid) {
             const uint4* kp = reinterpret_cast<const uint4*>(K + static_cast<int64_t>(j0 + lane) * D);
-            constexpr int KB = D / VE < 8 ? D / VE : 8;      // vectors of the row under way at a time
+            constexpr int KB = D / VE < 16 ? D / VE : 16;    // vectors of the row under way at a time
             for (int v0 = 0; v0 < D / VE; v0 += KB) {
                 uint4 kv[KB];
 #pragma unroll
@@ -144,15 +156,7 @@ __global__ void __launch_bounds__(kWarps * 32) prefix_generic_kernel(const Prefi
             p_s[warp][r][lane] = pr;
         }
         __syncwarp();
-        const int cnt = min(32, last - j0);
-        constexpr int VB = 8;                        // value rows under way at a time
         for (int b0 = 0; b0 < cnt; b0 += VB) {
-            float v[VB][DPL];
-#pragma unroll
-            for (int u = 0; u < VB; ++u)
-                if (b0 + u < cnt)
-#pragma unroll
-                    for (int c = 0; c < DPL; ++c) v[u][c] = as_float(V[static_cast<int64_t>(j0 + b0 + u) * D + lane + 32 * c]);
 #pragma unroll
             for (int u = 0; u < VB; ++u) {
                 if (b0 + u >= cnt) break;
@@ -163,6 +167,7 @@ __global__ void __launch_bounds__(kWarps * 32) prefix_generic_kernel(const Prefi
                     for (int c = 0; c < DPL; ++c) o[r][c] = fmaf(pr, v[u][c], o[r][c]);
                 }
             }
+            values(b0 + VB);
         }
         __syncwarp();
     }

@@ -62,9 +62,9 @@ __global__ void __launch_bounds__(kThreads) __cluster_dims__(kCluster, 1, 1) bui
     extern __shared__ int64_t smem[];
     __shared__ int64_t warp_sums[kThreads / 32];
     const int n = p.n, hkv = p.kv_heads, ctas = p.n_ctas;
-    // over the requests that hold a token ("held", in order): cost before each, request, length
-    int64_t* cost_before = smem;                                        // [n + 1]
-    int32_t* held_req = reinterpret_cast<int32_t*>(cost_before + n + 1); // [n]
+    // over the requests that hold a token ("held", in order): cost of all heads before each, request, length
+    int64_t* cost_before = smem;                                        // [n]
+    int32_t* held_req = reinterpret_cast<int32_t*>(cost_before + n);    // [n]
     int32_t* held_len = held_req + n;                                   // [n]
     // over all requests: first new token, committed length (-1: refused)
     int32_t* cu = held_len + n;                                         // [n + 1]
@@ -135,27 +135,29 @@ __global__ void __launch_bounds__(kThreads) __cluster_dims__(kCluster, 1, 1) bui
         const int r = static_cast<int>(pre >> 48);
         held_req[r] = tid * per + k;
         held_len[r] = add[k];
-        cost_before[r] = pre & ((int64_t(1) << 48) - 1);
+        cost_before[r] = (pre & ((int64_t(1) << 48) - 1)) * hkv;
         pre += (int64_t(1) << 48) + (add[k] + kTileTokens - 1) / kTileTokens + 1;
     }
-    if (tid == 0) cost_before[n_held] = req_cost;
     if (rank == 0 && bad) atomicOr(p.status, kStatusOverflow);
     __syncthreads();
 
     // ---- the shares' starts
     const int streams = n_held * hkv;
     const int64_t work = req_cost * hkv;
-    const int64_t share = max((work + ctas - 1) / ctas, static_cast<int64_t>(kMinShareTiles));
+    // (both below 2^41, so the rounded quotient's floor is the quotient's)
+    const int64_t share = max(static_cast<int64_t>(static_cast<double>(work + ctas - 1) / ctas), static_cast<int64_t>(kMinShareTiles));
     int64_t sums = 0;                                  // of this thread's starts: inner cuts (low), first ones (high)
     const int cper = (ctas + 1 + kThreads - 1) / kThreads;
     for (int c = tid * cper; c < min((tid + 1) * cper, ctas + 1); ++c) {
         const int64_t x = c * share;
         int q = streams, t = 0;
         if (x < work && c < ctas) {
-            const int r = upper_bound(cost_before, n_held, x / hkv) - 1;      // hkv * cost_before[r] <= x
+            const int r = upper_bound(cost_before, n_held, x) - 1;
             const int of = (held_len[r] + kTileTokens - 1) / kTileTokens;
-            const int64_t in = x - cost_before[r] * hkv;
-            const int h = static_cast<int>(in / (of + 1)), u = static_cast<int>(in - static_cast<int64_t>(h) * (of + 1));
+            const int64_t in = x - cost_before[r];     // < kv_heads * (of + 1)
+            const int h = in < (int64_t(1) << 32) ? static_cast<int>(static_cast<uint32_t>(in) / static_cast<uint32_t>(of + 1))
+                                                  : static_cast<int>(in / (of + 1));
+            const int u = static_cast<int>(in - static_cast<int64_t>(h) * (of + 1));
             q = r * hkv + h;
             t = u - 1;
             if (of < 2 * kMinPieceTiles) {             // never cut: to the nearer end
@@ -260,7 +262,7 @@ __global__ void __launch_bounds__(kThreads) __cluster_dims__(kCluster, 1, 1) bui
     }
 }
 
-int smem_bytes(int n, int ctas) { return 8 * (n + 1) + 4 * (4 * n + 1) + 4 * 4 * (ctas + 1); }
+int smem_bytes(int n, int ctas) { return 8 * n + 4 * (4 * n + 1) + 4 * 4 * (ctas + 1); }
 
 }  // namespace
 
