@@ -1142,13 +1142,13 @@ int32_t odma_decode_attention_prefix(odma_pool* pool, int32_t layer, const void*
             // Behind the prefix's kernel the launch need not wait: the tables, queries and slab rows were complete before
             // that kernel began (it waits for all work ahead of it), and it writes only the workspace.  So the tcgen05
             // kernel runs as a chained launch, or the other one asks for its first rows early.
-            const bool behind = splits > 0 && tensor;
+            const bool behind = splits > 0;
             const bool umma = uses_umma(pool, p.group, behind);
             p.chained = umma && behind ? 1 : 0;
             p.early_ok = behind ? 1 : 0;
             e = launch_tensor_decode(pool, pool->maps, p, kModeSlab, tables, s, nullptr, umma, nullptr, behind);
         } else {
-            e = launch_decode_generic(p, pool->dtype, tables->n_ctas, s);
+            e = launch_decode_generic(p, pool->dtype, tables->n_ctas, s, splits > 0);
         }
         if (e != cudaSuccess) return ODMA_ERR_CUDA;
     }

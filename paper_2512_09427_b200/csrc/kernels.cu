@@ -1037,6 +1037,8 @@ decode_generic_kernel(const DecodeParams p) {
             }
         }
     }
+    // A launch beside the kernel ahead ends after it (otherwise that kernel is complete already).
+    asm volatile("griddepcontrol.wait;" ::: "memory");
 }
 
 // =============================================================================================
@@ -1212,15 +1214,28 @@ void tc_shape_inst(int32_t ctas_per_sm, int32_t* stages, int32_t* q_slots) {
     *q_slots = std::min(kMaxQSlots, kMinQSlots + extra);
 }
 
+template <typename T, int DPL>
+cudaError_t launch_generic_inst(const DecodeParams& p, int n_ctas, cudaStream_t s, bool beside) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(n_ctas));
+    cfg.blockDim = dim3(kGenericWarps * 32);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = beside ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, decode_generic_kernel<T, DPL>, p);
+}
+
 template <typename T>
-cudaError_t launch_generic_t(const DecodeParams& p, int n_ctas, cudaStream_t s) {
+cudaError_t launch_generic_t(const DecodeParams& p, int n_ctas, cudaStream_t s, bool beside) {
     switch (p.head_dim) {
-        case 32: decode_generic_kernel<T, 1><<<n_ctas, kGenericWarps * 32, 0, s>>>(p); break;
-        case 64: decode_generic_kernel<T, 2><<<n_ctas, kGenericWarps * 32, 0, s>>>(p); break;
-        case 128: decode_generic_kernel<T, 4><<<n_ctas, kGenericWarps * 32, 0, s>>>(p); break;
-        default: return cudaErrorInvalidValue;
+        case 32: return launch_generic_inst<T, 1>(p, n_ctas, s, beside);
+        case 64: return launch_generic_inst<T, 2>(p, n_ctas, s, beside);
+        case 128: return launch_generic_inst<T, 4>(p, n_ctas, s, beside);
     }
-    return cudaGetLastError();
+    return cudaErrorInvalidValue;
 }
 
 }  // namespace
@@ -1256,9 +1271,9 @@ cudaError_t launch_decode_tc(const TensorMaps& maps, const DecodeParams& p, int 
     return cudaErrorInvalidValue;
 }
 
-cudaError_t launch_decode_generic(const DecodeParams& p, int dtype, int n_ctas, cudaStream_t stream) {
-    return dtype == ODMA_DTYPE_F32 ? launch_generic_t<float>(p, n_ctas, stream)
-                                   : launch_generic_t<__nv_bfloat16>(p, n_ctas, stream);
+cudaError_t launch_decode_generic(const DecodeParams& p, int dtype, int n_ctas, cudaStream_t stream, bool beside) {
+    return dtype == ODMA_DTYPE_F32 ? launch_generic_t<float>(p, n_ctas, stream, beside)
+                                   : launch_generic_t<__nv_bfloat16>(p, n_ctas, stream, beside);
 }
 
 cudaError_t launch_combine(const int4* combine, int n_combine, const float* part_o,

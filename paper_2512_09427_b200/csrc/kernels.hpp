@@ -102,7 +102,8 @@ bool umma_supported(int32_t head_dim, int32_t group, bool kv_fp8);
 cudaError_t launch_decode_umma(const TensorMaps& maps, const DecodeParams& p, int mode, int n_ctas,
                                cudaStream_t stream, const InlineLens* lens = nullptr, const SpanParams* span = nullptr,
                                bool defer = false, bool overlap = true);
-cudaError_t launch_decode_generic(const DecodeParams& p, int dtype, int n_ctas, cudaStream_t stream);
+// `beside`: the kernel ahead lets this one begin at once, and this one reads nothing that it writes (it still ends after it).
+cudaError_t launch_decode_generic(const DecodeParams& p, int dtype, int n_ctas, cudaStream_t stream, bool beside = false);
 bool generic_supported(int32_t head_dim);
 
 cudaError_t launch_combine(const int4* combine, int n_combine, const float* part_o,

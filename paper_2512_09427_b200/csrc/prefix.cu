@@ -82,6 +82,7 @@ __global__ void __launch_bounds__(kWarps * 32) prefix_generic_kernel(const Prefi
     __shared__ float mrg_o[kWarps][kRows][D];
     __shared__ float mrg_ml[kWarps][kRows][2];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");      // the requests' own parts run beside this
     const int head = blockIdx.y, rows = p.n * p.group, r0 = blockIdx.x * kRows;
     int first, last;
     split_range(p, blockIdx.z, first, last);
@@ -334,8 +335,9 @@ cudaError_t launch_generic_t(const PrefixParams& p, cudaStream_t s) {
 
 // Blocks along the prefix's keys: the number that minimises (waves of blocks) x (a block's time) + (what the
 // partial results cost), by measured figures in ns.  Tensor cores (one block per SM): 6,500 for a block's set-up,
-// queries and hand-over, and per step of 64 keys 1,100 with two row tiles, 900 with one, 600 when one row
-// tile's steps go to the two lanes in turn.  Plain ALUs (8 rows, four blocks per SM): 3,000 and 5,000 per tile
+// queries and hand-over, and per step of 64 keys 1,100 with two row tiles, 900 with one; when one row tile's steps
+// go to the two lanes in turn, 7,500 and 750 (it pays from four tiles of 128 keys per block on: 3 requests, 777
+// keys, 2 blocks: 14.1 us against 14.4; 7 blocks: 12.4 against 11.0).  Plain ALUs (8 rows, four blocks per SM): 3,000 and 5,000 per tile
 // of 128 keys.  A row's partial result costs its write and its read in the merge, 0.2.
 PrefixSplit prefix_split(int32_t rows, int32_t q_rows, int32_t kv_heads, int32_t len, int32_t sms, bool tensor) {
     const int64_t tiles = (len + kPrefixTile - 1) / kPrefixTile;
@@ -346,7 +348,9 @@ PrefixSplit prefix_split(int32_t rows, int32_t q_rows, int32_t kv_heads, int32_t
     for (int32_t s = 1; s <= std::min<int64_t>(tiles, kMaxPrefixSplits); ++s) {
         const int64_t waves = (blocks * s + room - 1) / room, each = (tiles + s - 1) / s;
         for (int32_t turn = 0; turn <= (tensor && rows <= 128 ? 1 : 0); ++turn) {
-            const int64_t block = !tensor ? 3000 + 5000 * each : 6500 + 2 * each * (turn ? 600 : rows <= 128 ? 900 : 1100);
+            const int64_t block = !tensor ? 3000 + 5000 * each
+                                  : turn    ? 7500 + 2 * each * 750
+                                            : 6500 + 2 * each * (rows <= 128 ? 900 : 1100);
             const int64_t parts = turn ? 2 * s : s, cost = waves * block + parts * q_rows / 5;
             if (cost < least) {
                 least = cost;
