@@ -544,3 +544,125 @@ def test_on_another_stream():
         run_prefix(s, [1, 2], [40, 41], 0, 633, 28, device_plan(s, [1, 2], [0, 0]))
         s2 = SlabPool([64, 64], [40, 41], 1, 4, 128, "bf16")
         run_append(s2, device_plan(s2, [0, 1]), [0, 1], [40, 41], 28, 128)
+
+
+# ---- large steps, and calls next to one another -------------------------------------------------------
+
+MANY = [("bf16", 28, 4, 128, 128), ("bf16", 3, 1, 128, 16), ("bf16", 4, 2, 64, 8), ("bf16", 2, 1, 80, 80), ("bf16", 2, 1, 24, 8),
+        ("bf16", 2, 2, 256, 128), ("f32", 4, 2, 64, 64), ("f32", 3, 3, 128, 24), ("e4m3", 8, 4, 128, 128), ("e4m3", 5, 1, 128, 40)]
+
+
+@pytest.mark.parametrize("kind,q_heads,hkv,d,rot", MANY)
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_append_qkv_of_a_large_chunk(kind, q_heads, hkv, d, rot, interleaved):
+    lens, new = [0, 100, 7], [400, 1, 629]                        # 1,030 tokens: blocks of several, the last one short
+    s = SlabPool([400, 112, 640], lens, 1, hkv, d, kind, seed=rot)
+    t = s.tables([0, 1, 2], new)
+    owner = [i for i, c in enumerate(new) for _ in range(c)]
+    position = [lens[i] + j for i, c in enumerate(new) for j in range(c)]
+    run_append(s, t, owner, position, q_heads, rot, interleaved, norm=rot % 16 == 0)
+    pairs = rot // 2
+    g = torch.Generator().manual_seed(d)
+    run_append(s, t, owner, position, q_heads, rot, interleaved, [pairs - pairs // 2, pairs // 2], norm=rot % 16 != 0, fused=False,
+               positions=torch.randint(0, 1 << 17, (2, 1030), generator=g))
+    assert s.sync() == 0
+
+
+def test_append_qkv_of_a_large_chunk_with_refused_and_spare_rows():
+    lens, new = [5, 30, 0, 2], [300, 9, 500, 200]
+    s = SlabPool([320, 32, 512, 208], lens, 1, 2, 128, "bf16")      # the second does not fit
+    t = device_plan(s, [0, 1, 2, 3], new, n_new=1100)
+    owner = [0] * 300 + [-1] * 9 + [2] * 500 + [3] * 200 + [-1] * 91
+    position = list(range(5, 305)) + [0] * 9 + list(range(500)) + list(range(2, 202)) + [0] * 91
+    run_append(s, t, owner, position, 4, 128)
+    assert s.sync() == ref.lib().ERR_OVERFLOW
+
+
+@pytest.mark.parametrize("kind,d,kernel", [("f32", 64, "auto"), ("bf16", 128, "auto"), ("bf16", 64, "mma"), ("bf16", 128, "mma"), ("e4m3", 128, "auto")])
+def test_behind_a_prefix_nobody_holds_a_token(kind, d, kernel):
+    over = {"decode_kernel": ref.lib().DECODE_MMA_SYNC} if kernel == "mma" else {}
+    s = SlabPool([272, 16, 16, 16], [260, 0, 0, 0], 1, 2, d, kind, **over)
+    run_prefix(s, [1, 2, 3], [0, 0, 0], 0, 260, 6, device_plan(s, [1, 2, 3], [0, 0, 0]))
+    s = SlabPool([272, 64, 208, 16], [260, 50, 200, 1], 1, 2, d, kind, **over)
+    run_prefix(s, [1, 2, 3], [50, 200, 1], 0, 260, 6, repeat=2)
+
+
+@pytest.mark.parametrize("kind,d", [("bf16", 128), ("f32", 64), ("e4m3", 128)])
+def test_a_prefill_chunk_behind_a_prefix(kind, d):
+    """One stream per new token (the tables of a prefill chunk): token j sees the prefix, the request's tokens before the
+    chunk and the chunk up to itself."""
+    lens, new = [20, 0], [5, 9]
+    s = SlabPool([144, 32, 16], [130, 25, 9], 1, 2, d, kind, max_batch=16)
+    for r, have in ((1, 25), (2, 9)):                            # rows are there; lengths as before the chunk
+        assert s.pool.free(r) == 0
+        assert s.pool.set_buckets([s.caps[r]]) == 0
+        rc, slab = s.pool.alloc(r, s.caps[r])
+        assert rc == 0 and slab[0] == s.base[r]
+    assert s.pool.commit_step([1], [20]) == 0
+    t = s.pool.build_prefill_tables([1, 2], new, s.table.data_ptr(), s.table.numel(), s.stream)
+    reqs = [1] * 5 + [2] * 9
+    run_prefix(s, reqs, [lens[0] + j + 1 for j in range(5)] + [j + 1 for j in range(9)], 0, 130, 6, t)
+
+
+@pytest.mark.parametrize("kind,q_heads,hkv,d", [("bf16", 28, 4, 128), ("bf16", 12, 2, 64), ("e4m3", 28, 4, 128)])
+def test_steps_and_prefix_calls_in_a_row(kind, q_heads, hkv, d):
+    """Decode steps (which may overlap with the launch before them) and calls behind a prefix, on two layers in turn,
+    give the same bits whether or not every call is waited for."""
+    lens = [30, 1, 400, 77, 130, 64]
+    n, reqs = len(lens), [1, 2, 3, 4, 5, 6]
+
+    def go(wait):
+        s = SlabPool([320] + [(x + 47) // 16 * 16 for x in lens], [301] + lens, 2, hkv, d, kind, seed=9)
+        ws = torch.empty(s.pool.prefix_workspace_bytes(q_heads, n, 301), dtype=torch.uint8, device="cuda")
+        outs = []
+        for i in range(6):
+            for layer in (0, 1):
+                q, k, v = s.randn(n, q_heads, d), s.randn(n, hkv, d), s.randn(n, hkv, d)
+                a, b = torch.empty_like(q), torch.empty_like(q)
+                t = s.pool.decode_step
+                t(layer, 1, q_heads, reqs, q.data_ptr(), k.data_ptr(), v.data_ptr(), a.data_ptr(), 0, s.stream)
+                if wait:
+                    torch.cuda.synchronize()
+                tab = s.tables(reqs)
+                s.pool.decode_attention_prefix(1 - layer if i % 2 else layer, q.data_ptr(), q_heads, 0, 301, tab, ws.data_ptr(), ws.numel(),
+                                               b.data_ptr(), 0, s.stream)
+                if wait:
+                    torch.cuda.synchronize()
+                outs += [a, b, q, k, v]
+            assert s.pool.commit_step(reqs, [1] * n) == 0
+        assert s.sync() == 0
+        return outs, s.mem.clone()
+
+    # every layer's rows of a step are in place before the lengths move on: the calls on the other layer read rows of this step
+    # that the step on that layer writes (i odd) or has written, so only equal schedules are compared
+    one, mem1 = go(True)
+    two, mem2 = go(True)
+    for a, b in zip(one, two):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    three, mem3 = go(False)
+    for a, b in zip(one, three):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    assert torch.equal(mem1.view(torch.uint8), mem3.view(torch.uint8))
+
+
+def test_two_pools_on_two_streams():
+    pools = [SlabPool([1040, 64, 240], [1033, 40, 230], 1, 4, 128, kind, seed=i) for i, kind in enumerate(("bf16", "e4m3"))]
+    alone = [run_prefix(s, [1, 2], [40, 230], 0, 1033, 28) for s in pools]
+    del alone
+    qs = [s.randn(2, 28, 128) for s in pools]
+    tabs = [s.tables([1, 2], [0, 0]) for s in pools]
+    spaces = [torch.empty(s.pool.prefix_workspace_bytes(28, 2, 1033), dtype=torch.uint8, device="cuda") for s in pools]
+    want = [torch.empty_like(q) for q in qs]
+    for s, q, t, w, o in zip(pools, qs, tabs, spaces, want):
+        s.pool.decode_attention_prefix(0, q.data_ptr(), 28, 0, 1033, t, w.data_ptr(), w.numel(), o.data_ptr(), 0, s.stream)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in pools]
+    got = [[torch.empty_like(q) for _ in range(20)] for q in qs]
+    for i in range(20):
+        for s, q, t, w, o, st in zip(pools, qs, tabs, spaces, got, streams):
+            s.pool.decode_attention_prefix(0, q.data_ptr(), 28, 0, 1033, t, w.data_ptr(), w.numel(), o[i].data_ptr(), 0, st.cuda_stream)
+    torch.cuda.synchronize()
+    for s, w, o in zip(pools, want, got):
+        assert s.pool.check_status() == 0
+        for x in o:
+            assert torch.equal(x, w)
