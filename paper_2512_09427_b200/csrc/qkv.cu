@@ -11,9 +11,11 @@
 // in fp32: a position of 10^6 times an fp32 frequency keeps no digits of the turn in 32 bits.
 //
 // Each input element is read once and each output element written once: a chunk of 8,192 tokens of the
-// 28 + 4 + 4-head layer moves 151 MB.  What bounds it in practice is instruction issue (a row of 128
-// elements over 16 lanes of 8 took 245 instructions per two rows and 43 us; over 8 lanes of 16 with a
-// token's addresses, turns and weights in registers ISSUE).  A token's rot_dim / 2 sines and cosines are
+// 28 + 4 + 4-head layer moves 151 MB, 23.4 us at the measured copy rate; the kernel takes 35.5 us (4.3 TB/s).
+// Beside the memory it is instruction issue that bounds it (59 % of the issue slots): a row of 128
+// elements over 16 lanes of eight took 245 instructions per warp and 43 us, over 8 lanes of sixteen, with a
+// token's addresses, turns and weights in registers and packed arithmetic, 35.5.  One token, or 256: 3.0
+// and 3.8 us, a chain of latencies (owner, position, angle, row).  A token's rot_dim / 2 sines and cosines are
 // computed once, into shared memory, under the latency of the first row loads, and serve all its heads.
 // A row is held by D / 16 (D / 8) lanes, laid out so that both elements of a pair sit in the same lane
 // (pairs (i, i + rot_dim / 2): a run of eight (four) of each half; adjacent pairs: a run of twice that);
@@ -27,7 +29,7 @@ using namespace dev;
 
 constexpr int kMaxThreads = 384;
 // Tokens per block: one while that fills the GPU (a token's way through a block, some 3 us, is all a small step costs),
-// several for more, whose rows then stream behind one another while the next tokens' angles are there already.
+// several for more, whose rows then stream behind one another (chunk of 8,192: 50 us with one per block, 43 with four).
 constexpr int kTokens = 4, kManyTokens = 1024, kManyThreads = 128, kManyBlocks = 5;
 
 // N consecutive elements of a row, in pairs of two.
@@ -273,7 +275,7 @@ cudaError_t launch_t(const QkvParams& p, cudaStream_t stream) {
         launch_tok<T, N, QUANT, 8>(p, stream);
     else if (lanes <= 16)
         launch_tok<T, N, QUANT, 16>(p, stream);
-    else
+    else if constexpr (N == 4)                      // heads of more than 128 elements, eight to a lane
         launch_tok<T, N, QUANT, 32>(p, stream);
     return cudaGetLastError();
 }
