@@ -23,11 +23,15 @@
 // below 256, which bf16 relative to the fp32 accumulator does not mind, and O is rescaled in tensor
 // memory only then.  P is rounded to bf16 for the product (half a step: 2^-9 to 2^-8 of a weight, random
 // in sign over the keys); sums, maxima and O are fp32.
-// 32,768 keys and 7,168 rows (120 GFLOP): 115 us, 1.05 PFLOP/s (0.62 of the measured burst rate), some 1.07 us per step
-// of 64 keys and 256 rows; the products alone would take 0.68 (the second one's instructions at the pipe's rate,
-// the first one's, 64 keys wide, at shared memory's), the exponentials 0.55, and the GPU is at its power
-// limit (985 W) meanwhile.  A block's set-up, queries and hand-over cost 6.5 us, of which the 128 KB of its partial
-// results are 2.4: that is what short prefixes pay for.
+//
+// What bounds it: the tensor pipe.  32,768 keys and 7,168 rows (120 GFLOP): 110 to 120 us, 1.0 to 1.1 PFLOP/s
+// (0.62 of the measured burst rate; the GPU sits at its power limit, 985 W), 1,570 cycles per step of 64 keys
+// and 256 rows.  An instruction takes 64 cycles, the first product's, 64 keys wide, no less than one of 128 keys
+// (2 x (8 + 4) x 64 = 1,536); with a quarter of the first product's instructions the call took 124 us instead of
+// 140, of the second's 130, without the exponentials 132, without loads 138.  Steps of 128 keys would halve the
+// first product's count and leave one S buffer per lane, whose chain of softmax and products is about as long.  A
+// block's set-up, queries and hand-over cost 6.5 us, of which the 128 KB of its partial results are 2.4: that is what
+// short prefixes pay for.
 #include "odma.h"
 #include "tcgen05.cuh"
 
