@@ -52,7 +52,7 @@ constexpr float kRescaleAbove = 8.f;
 constexpr int kQHalfBytes = kM * 128;               // 64 elements of a lane's queries
 constexpr int kHalfBytes = kStep * 128;             // 64 elements of a step's keys or values
 // barriers
-constexpr int kBarFull = 0, kBarEmpty = kMaxStages, kBarQ = 2 * kMaxStages, kBarP = kBarQ + 2, kBarS = kBarP + 4,
+constexpr int kBarFull = 0, kBarEmpty = kMaxStages, kBarP = 2 * kMaxStages, kBarS = kBarP + 4,
               kBarPv = kBarS + 4, kBarO = kBarPv + 2, kBarDrain = kBarO + 2, kNumBars = kBarDrain + 2;   // S, P: [lane][buffer]
 
 template <int D>
@@ -176,8 +176,8 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
     const bool lane1 = in_turn || r0 + kM < rows;    // is there a second lane?
     const int blocks = in_turn ? p.splits >> 1 : p.splits;      // splits of the keys over the blocks, in tiles of 128
     const int all_tiles = (p.len + kPrefixTile - 1) / kPrefixTile;
-    const int k0 = static_cast<int>(static_cast<int64_t>(all_tiles) * blockIdx.z / blocks) * kPrefixTile;
-    const int k1 = min(p.len, static_cast<int>(static_cast<int64_t>(all_tiles) * (blockIdx.z + 1) / blocks) * kPrefixTile);
+    const int z = static_cast<int>(blockIdx.z);      // below 128, and tiles below 2^24: no product leaves 32 bits
+    const int k0 = all_tiles * z / blocks * kPrefixTile, k1 = min(p.len, all_tiles * (z + 1) / blocks * kPrefixTile);
     const int steps = (k1 - k0 + kStep - 1) / kStep; // of the block; a lane takes all of them, or every second one
     const int turn = in_turn ? 2 : 1, ahead = 2 * turn;         // K of a step is asked for `ahead` steps before its V
     auto lane_steps = [&](int L) { return in_turn ? (steps - L + 1) / 2 : steps; };
@@ -186,11 +186,11 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
     bool ok = true;
     auto out_row = [&](int r) { return (r / p.group) * p.q_heads + head * p.group + r % p.group; };    // row of q and of a partial result
 
-    // ---- set-up, the roles side by side: barriers and the first loads; tensor memory; the queries' loads
+    // ---- set-up, the roles side by side: barriers and the first loads; tensor memory; the queries
     uint32_t issued = 0;
     auto load = [&](bool is_v, int u) {              // the producer's next stage
         const uint32_t stage = issued % STAGES, use = issued / STAGES;
-        ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(kBarEmpty + stage), (use & 1u) ^ 1u, abort_flag, p.status, limit));
+        if (use > 0) ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(kBarEmpty + stage), (use & 1u) ^ 1u, abort_flag, p.status, limit));
         if (!ok) return;
         if (lane == 0) mbar_expect_tx(bar(kBarFull + stage), static_cast<uint32_t>(Cfg::kStageBytes));
         __syncwarp();
@@ -202,11 +202,10 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
     constexpr int QCH = D / 8;                       // 16-byte chunks of a query row
     constexpr int QLOADS = kM * QCH / kLaneThreads;  // per thread of a lane
     constexpr int QROWS = 32 / QCH;                  // rows per warp and load
-    uint4 qv[QLOADS];
     if (warp == kProducerWarp) {
         for (int i = lane; i < kNumBars; i += 32) {
-            const bool softmax = i >= kBarQ && i < kBarS;                        // arrivals of a lane's softmax warps
-            const bool shared = i >= kBarEmpty && i < kBarQ && lane1;            // both lanes hand every stage back
+            const bool softmax = i >= kBarP && i < kBarS;                        // arrivals of a lane's softmax warps
+            const bool shared = i >= kBarEmpty && i < kBarP && lane1;            // both lanes hand every stage back
             mbar_init(bar(i), softmax ? kLaneThreads / 32u : shared ? 2u : 1u);
         }
         if (lane == 0) *abort_flag = 0;
@@ -218,16 +217,25 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u)
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    } else if (warp < kSoftmaxWarps) {
-        // a warp loads 16 of its lane's 128 rows, QROWS at a time; one thread works out one row's place
-        const int g0 = r0 + (in_turn ? 0 : (warp >> 3) * kM) + (warp & 7) * (QROWS * QLOADS);
+    } else if (warp < kSoftmaxWarps && (warp < 8 || (lane1 && !in_turn))) {
+        // Queries to shared memory, in the swizzled order: a warp takes 16 of its lane's 128 rows, QROWS at a time, all
+        // loads before the first store; one thread works out one row's place.
+        const int w0 = (warp & 7) * (QROWS * QLOADS), g0 = r0 + (warp >> 3) * kM + w0;
         const int mine = out_row(min(g0 + (lane & (QROWS * QLOADS - 1)), rows - 1));
+        uint4 qv[QLOADS];
 #pragma unroll
         for (int i = 0; i < QLOADS; ++i) {
             const int r = i * QROWS + lane / QCH, at = __shfl_sync(0xFFFFFFFFu, mine, r);
             qv[i] = make_uint4(0u, 0u, 0u, 0u);      // rows behind the last are zero
             if (g0 + r < rows) qv[i] = __ldg(static_cast<const uint4*>(p.q) + static_cast<int64_t>(at) * QCH + lane % QCH);
         }
+        uint8_t* dst = qbuf + (warp >> 3) * Cfg::kQBytes;
+#pragma unroll
+        for (int i = 0; i < QLOADS; ++i) {
+            const int r = w0 + i * QROWS + lane / QCH, c = lane % QCH;
+            *reinterpret_cast<uint4*>(dst + (c >> 3) * kQHalfBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = qv[i];
+        }
+        fence_proxy_async();
     }
     tc_fence_before();
     __syncthreads();
@@ -317,7 +325,6 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
                 if (elected && ok) mbar_arrive(bar(kBarEmpty + stage));
                 __syncwarp();
             };
-            wait(bar(kBarQ + (in_turn ? 0 : L)), 0);
             for (int u = 0; u < min(ahead, steps) && ok; ++u) {
                 const uint32_t ks = wait_stage();
                 if (u % turn != mine)
@@ -358,17 +365,6 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
         const int row = (warp & 3) * 32 + lane;      // of the lane's tile
         const int g_row = r0 + (in_turn ? 0 : L * kM) + row;
         const int pair_id = 1 + L * 4 + (warp & 3);  // barrier of the row's two warps
-        if (L == 0 || (lane1 && !in_turn)) {         // queries to shared memory, in the swizzled order
-            uint8_t* dst = qbuf + L * Cfg::kQBytes;
-#pragma unroll
-            for (int i = 0; i < QLOADS; ++i) {
-                const int r = (warp & 7) * (QROWS * QLOADS) + i * QROWS + lane / QCH, c = lane % QCH;
-                *reinterpret_cast<uint4*>(dst + (c >> 3) * kQHalfBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = qv[i];
-            }
-            fence_proxy_async();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar(kBarQ + L));
-        }
         const uint32_t t_s = tmem + (static_cast<uint32_t>(warp & 3) << 21) + static_cast<uint32_t>(L) * 256u, t_o = t_s + 128u;
         const float scale = p.scale_log2;
         float m = -INFINITY, l = 0.f;                // reference (log2 units, the same in a row's two threads) and sum
@@ -448,21 +444,23 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
             const uint32_t st = static_cast<uint32_t>(L * kM + row) * PITCH;
             if (side == 1) xch[L * kM + row] = l;
             if (ok) {
+                uint32_t o[D / 32][16];
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c) {
-                    uint32_t o[16];
                     if (own > 0) {
-                        tmem_ld_row16(t_o + static_cast<uint32_t>(side * (D / 2) + 16 * c), o);
-                        tmem_wait_ld();
+                        tmem_ld_row16(t_o + static_cast<uint32_t>(side * (D / 2) + 16 * c), o[c]);
                     } else {
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) o[i] = 0u;
+                        for (int i = 0; i < 16; ++i) o[c][i] = 0u;
                     }
+                }
+                tmem_wait_ld();
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         *reinterpret_cast<uint4*>(smem + st + (side * (D / 2) + 16 * c + 4 * i) * 4) =
-                            make_uint4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-                }
+                            make_uint4(o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]);
             }
             fence_proxy_async();
             lane_sync(pair_id, 64);
