@@ -361,7 +361,7 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
         mbar_wait_slow(bar(kBarDrain + L), 0, nullptr, p.status, limit / 4 + 1);
     } else {
         // ------------------------------------------------------------------ softmax
-        const int L = warp >> 3, side = (warp >> 2) & 1;     // lane; left or right 64 keys of a tile
+        const int L = warp >> 3, side = (warp >> 2) & 1;     // lane; left or right half of a step's keys
         const int row = (warp & 3) * 32 + lane;      // of the lane's tile
         const int g_row = r0 + (in_turn ? 0 : L * kM) + row;
         const int pair_id = 1 + L * 4 + (warp & 3);  // barrier of the row's two warps
