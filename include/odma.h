@@ -400,7 +400,8 @@ int32_t odma_decode_attention(odma_pool* pool, int32_t layer, const void* q, int
  * workspace: device, 256-byte aligned, the caller's: partial results of the prefix's splits (and, for an
  * 8-bit pool, the prefix as bf16).  odma_prefix_workspace_bytes gives the size for n requests at the
  * best number of splits (0 for a bad shape); with less, down to one split, the call uses fewer.
- * Calls that overlap on the GPU need workspaces of their own.  A captured call keeps the place of the
+ * Calls of one pool are ordered, as everywhere, and may share a workspace; calls of two pools that overlap on
+ * the GPU need one each.  A captured call keeps the place of the
  * prefix's slab and prefix_len: capture again when that request has moved or been freed. */
 uint64_t odma_prefix_workspace_bytes(const odma_pool* pool, int32_t q_heads, int32_t n, int32_t prefix_len);
 int32_t odma_decode_attention_prefix(odma_pool* pool, int32_t layer, const void* q, int32_t q_heads,
