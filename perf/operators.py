@@ -282,8 +282,9 @@ def _prepare_tables(case, seed):
     }
     if own:
         geometry = {"kv_heads": hkv, "head_dim": 64, "dtype": "bf16"}
-        state["mem"] = torch.empty(at * hkv * 2 * 64, dtype=torch.bfloat16, device="cuda")
-        pool = _handle(geometry, state["mem"], at, [_up16(max(cap))], n, 8)
+        room = max(at, 16)                # slabs may all be empty; a pool has room for some tokens
+        state["mem"] = torch.empty(room * hkv * 2 * 64, dtype=torch.bfloat16, device="cuda")
+        pool = _handle(geometry, state["mem"], room, [max(16, _up16(max(cap)))], n, 8)
         state["table"] = torch.empty(pool.tables_bytes(n), dtype=torch.uint8, device="cuda")
         state["next"] = torch.empty(n, **dev)
         state["slots"] = torch.empty(state["n_new"], **dev)
