@@ -282,7 +282,8 @@ int32_t odma_build_tables(odma_pool* pool, const uint64_t* reqs, const int32_t* 
  * requests on the device): one kernel, no host planning, no copy.
  * odma_slab_table writes the slabs of n live requests to d_slabs (device, [n][2] int32: base,
  * capacity; 8-byte aligned) and, unless d_len is NULL, their committed lengths to d_len (device,
- * [n]), with asynchronous copies; to be repeated when the batch or a slab changes.
+ * [n]), with asynchronous copies; to be repeated when the batch or a slab changes (not captured:
+ * ODMA_ERR_INVALID on a stream that is being captured).
  * odma_build_tables_device reads d_slabs, d_len (tokens before the step) and d_n_new ([n], tokens
  * of the step; NULL: one each, n_new_total = n) and writes
  *   d_table      the table described at odma_tables (16-byte aligned, table_bytes >=

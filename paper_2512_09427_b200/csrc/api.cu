@@ -724,6 +724,10 @@ int32_t odma_slab_table(odma_pool* pool, const uint64_t* reqs, int32_t n, int32_
     if ((reinterpret_cast<uintptr_t>(d_slabs) & 7u) != 0 || (reinterpret_cast<uintptr_t>(d_len) & 3u) != 0) return ODMA_ERR_INVALID;
     for (int32_t i = 0; i < n; ++i)
         if (!pool->alloc.find(reqs[i])) return ODMA_ERR_UNKNOWN_REQ;
+    // a captured copy would read this staging slot again at every replay, when later calls have filled it
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(as_stream(stream), &capture) != cudaSuccess) return ODMA_ERR_CUDA;
+    if (capture != cudaStreamCaptureStatusNone) return ODMA_ERR_INVALID;
     Staging& st = pool->staging[pool->staging_next];
     pool->staging_next = (pool->staging_next + 1) % kStagingSlots;
     if (st.in_flight && cudaEventSynchronize(st.done) != cudaSuccess) return ODMA_ERR_CUDA;

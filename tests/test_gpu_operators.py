@@ -535,6 +535,27 @@ def test_decode_loop_captured_once_and_replayed(kind, q_heads, hkv, d):
     assert s.pool.commit_step(reqs, [steps] * n) == 0
 
 
+def test_slab_table_is_not_captured():
+    odma = ref.lib()
+    s = SlabPool([64, 32], [40, 7], 1, 2, 64, "bf16")
+    slabs, length = dev([[-1, -1], [-1, -1]]), dev([-1, -1])
+    filled = torch.zeros(4, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        with pytest.raises(odma.OdmaError) as refusal:
+            s.pool.slab_table([0, 1], slabs.data_ptr(), length.data_ptr(), torch.cuda.current_stream().cuda_stream)
+        assert refusal.value.code == odma.ERR_INVALID
+        filled.fill_(1.0)
+    graph.replay()                                                # the capture has gone on
+    torch.cuda.synchronize()
+    assert filled.tolist() == [1.0] * 4 and length.tolist() == [-1, -1]
+    for _ in range(8):                                            # and so do calls outside it, over every staging slot
+        s.pool.slab_table([0, 1], slabs.data_ptr(), length.data_ptr(), s.stream)
+    torch.cuda.synchronize()
+    assert slabs.tolist() == [[0, 64], [64, 32]] and length.tolist() == [40, 7]
+
+
 def test_on_another_stream():
     s = SlabPool([640, 64, 64], [633, 40, 41], 1, 4, 128, "bf16")
     torch.cuda.synchronize()
