@@ -479,7 +479,8 @@ int32_t odma_pool_create(void* dev_base, uint64_t bytes, int32_t layers, int32_t
                   cudaMalloc(&p->d_out, qb) == cudaSuccess && cudaMalloc(&p->d_k_new, kb) == cudaSuccess &&
                   cudaMalloc(&p->d_v_new, kb) == cudaSuccess &&
                   cudaMalloc(&p->d_step_table, static_cast<size_t>(p->table_words_max) * 4) == cudaSuccess &&
-                  cudaMemset(p->d_status, 0, 4) == cudaSuccess;
+                  cudaMemset(p->d_status, 0, 4) == cudaSuccess &&
+                  cudaStreamSynchronize(cudaStreamLegacy) == cudaSuccess;     // the first call may come on any stream
         if (ok) {
             p->part_o_floats = po / 4;
             p->part_ml_floats = pm / 4;
@@ -1328,13 +1329,19 @@ int32_t odma_decode_attention_static(const odma_pool* pool, const void* dev_base
 int32_t odma_check_status(odma_pool* pool, void* stream) {
     if (!pool || !pool->dev_base) return ODMA_ERR_INVALID;
     if (cudaStreamSynchronize(as_stream(stream)) != cudaSuccess) return ODMA_ERR_CUDA;
+    // read and cleared on `stream` itself, and waited for: the caller's next launch there finds everything in place,
+    // and no other stream is waited for
     uint32_t word = 0;
-    if (cudaMemcpy(&word, pool->d_status, 4, cudaMemcpyDeviceToHost) != cudaSuccess) return ODMA_ERR_CUDA;
+    cudaStream_t s = as_stream(stream);
+    if (cudaMemcpyAsync(&word, pool->d_status, 4, cudaMemcpyDeviceToHost, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess)
+        return ODMA_ERR_CUDA;
     if (word != 0) {
-        // a kernel that gave up may have left split streams half counted
-        if (cudaMemset(pool->d_status, 0, 4) != cudaSuccess ||
-            cudaMemset(pool->d_counters, 0, static_cast<size_t>(pool->slots_max) * 8) != cudaSuccess)
+        if (cudaMemsetAsync(pool->d_status, 0, 4, s) != cudaSuccess) return ODMA_ERR_CUDA;
+        // a kernel that gave up may have left split streams half counted (a refused request has not)
+        if ((word & kStatusTimeout) &&
+            cudaMemsetAsync(pool->d_counters, 0, static_cast<size_t>(pool->slots_max) * 8, s) != cudaSuccess)
             return ODMA_ERR_CUDA;
+        if (cudaStreamSynchronize(s) != cudaSuccess) return ODMA_ERR_CUDA;
     }
     if (word & kStatusTimeout) return ODMA_ERR_TIMEOUT;
     return (word & kStatusOverflow) ? ODMA_ERR_OVERFLOW : ODMA_OK;
