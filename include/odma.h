@@ -472,7 +472,8 @@ int32_t odma_decode_attention_static(const odma_pool* pool, const void* dev_base
 
 /* Synchronises `stream` and returns the device status word as an error code (ODMA_OK,
  * ODMA_ERR_TIMEOUT, ODMA_ERR_OVERFLOW for a request that odma_build_tables_device refused, or
- * ODMA_ERR_CUDA for a failed stream), clearing it.  Work on other streams is not waited for. */
+ * ODMA_ERR_CUDA for a failed stream), clearing what it reports: with both set, a call returns
+ * ODMA_ERR_TIMEOUT and the next one ODMA_ERR_OVERFLOW.  Work on other streams is not waited for. */
 int32_t odma_check_status(odma_pool* pool, void* stream);
 
 /* Failure detection, exercised without a fault: launches a one-thread kernel whose only wait

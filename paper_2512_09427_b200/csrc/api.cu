@@ -1335,16 +1335,15 @@ int32_t odma_check_status(odma_pool* pool, void* stream) {
     cudaStream_t s = as_stream(stream);
     if (cudaMemcpyAsync(&word, pool->d_status, 4, cudaMemcpyDeviceToHost, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess)
         return ODMA_ERR_CUDA;
-    if (word != 0) {
-        if (cudaMemsetAsync(pool->d_status, 0, 4, s) != cudaSuccess) return ODMA_ERR_CUDA;
-        // a kernel that gave up may have left split streams half counted (a refused request has not)
-        if ((word & kStatusTimeout) &&
-            cudaMemsetAsync(pool->d_counters, 0, static_cast<size_t>(pool->slots_max) * 8, s) != cudaSuccess)
-            return ODMA_ERR_CUDA;
-        if (cudaStreamSynchronize(s) != cudaSuccess) return ODMA_ERR_CUDA;
-    }
-    if (word & kStatusTimeout) return ODMA_ERR_TIMEOUT;
-    return (word & kStatusOverflow) ? ODMA_ERR_OVERFLOW : ODMA_OK;
+    if (word == 0) return ODMA_OK;
+    // the bit that is reported, and no other: the next call tells of the rest
+    const bool timeout = (word & kStatusTimeout) != 0;
+    if (launch_clear_status(pool->d_status, timeout ? kStatusTimeout : word, s) != cudaSuccess) return ODMA_ERR_CUDA;
+    // a kernel that gave up may have left split streams half counted (a refused request has not)
+    if (timeout && cudaMemsetAsync(pool->d_counters, 0, static_cast<size_t>(pool->slots_max) * 8, s) != cudaSuccess)
+        return ODMA_ERR_CUDA;
+    if (cudaStreamSynchronize(s) != cudaSuccess) return ODMA_ERR_CUDA;
+    return timeout ? ODMA_ERR_TIMEOUT : ODMA_ERR_OVERFLOW;
 }
 
 int32_t odma_read_probe(odma_pool* pool, int32_t layer, int32_t q_heads, const odma_tables* tables,

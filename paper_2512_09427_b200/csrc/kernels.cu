@@ -1133,6 +1133,8 @@ __global__ void __launch_bounds__(256) scatter_pages_kernel(const ScatterPagesPa
     }
 }
 
+__global__ void clear_status_kernel(uint32_t* status, uint32_t bits) { atomicAnd(status, ~bits); }
+
 __global__ void wait_selftest_kernel(uint32_t* status, int64_t limit_ns) {
     __shared__ uint64_t bar;
     __shared__ int abort_flag;
@@ -1353,6 +1355,11 @@ cudaError_t launch_decode_static(DecodeParams p, int dtype, int n_ctas, const in
     if (e != cudaSuccess) return e;
     return launch_combine(combine, n_combine, p.part_o, p.part_ml, p.out, p.lse, p.group, p.head_dim,
                           p.q_heads, dtype, stream);
+}
+
+cudaError_t launch_clear_status(uint32_t* status, uint32_t bits, cudaStream_t stream) {
+    clear_status_kernel<<<1, 1, 0, stream>>>(status, bits);
+    return cudaGetLastError();
 }
 
 cudaError_t launch_wait_selftest(uint32_t* status, int64_t limit_ns, cudaStream_t stream) {

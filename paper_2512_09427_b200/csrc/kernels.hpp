@@ -251,6 +251,8 @@ cudaError_t launch_decode_static(DecodeParams p, int dtype, int n_ctas, const in
 
 // A one-thread kernel that waits on a barrier nobody signals, for at most limit_ns, then
 // sets the timeout bit: exercises the bounded-wait path without hanging anything.
+// Takes `bits` out of the status word.
+cudaError_t launch_clear_status(uint32_t* status, uint32_t bits, cudaStream_t stream);
 cudaError_t launch_wait_selftest(uint32_t* status, int64_t limit_ns, cudaStream_t stream);
 
 }  // namespace odma

@@ -72,3 +72,16 @@ def test_split_streams_right_behind_a_refusal(kernel):
         torch.cuda.synchronize()
         assert torch.equal(out, want), i
     assert s.pool.check_status(side) == odma.OK
+
+
+@pytest.mark.parametrize("refused_first", [False, True])
+def test_a_timeout_does_not_hide_a_refusal(refused_first):
+    odma = ref.lib()
+    s = SlabPool([64, 16], [40, 3], 1, 2, 64, "bf16")
+    refuse = Refusal(s)
+    if refused_first:
+        refuse(s.stream)
+    assert s.pool.selftest_timeout(5, s.stream) == odma.OK
+    if not refused_first:
+        refuse(s.stream)
+    assert [s.pool.check_status(s.stream) for _ in range(3)] == [odma.ERR_TIMEOUT, odma.ERR_OVERFLOW, odma.OK]
