@@ -165,9 +165,6 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
     auto bar = [&](int i) { return bar0 + 8u * static_cast<uint32_t>(i); };
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int64_t limit = p.wait_limit_ns;
-    // The kernel behind this one (the requests' own parts) reads nothing that this one or the one ahead of it writes: its
-    // blocks may begin on every SM that this one leaves idle or is done with.
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     // the block's work
     const int head = blockIdx.y;
@@ -217,6 +214,11 @@ prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u)
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        // The kernel behind this one (the requests' own parts) reads nothing that this one or the one ahead of it writes: its
+        // blocks may begin on every SM that this one leaves idle or is done with.  They begin once every block of this
+        // kernel has come here, and so holds its tensor memory: theirs keep their columns until this kernel has ended, and a
+        // block of this one that still waited for columns on the same SM would never end.
+        asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     } else if (warp < kSoftmaxWarps && (warp < 8 || (lane1 && !in_turn))) {
         // Queries to shared memory, in the swizzled order: a warp takes 16 of its lane's 128 rows, QROWS at a time, all
         // loads before the first store; one thread works out one row's place.
