@@ -372,9 +372,10 @@ typedef struct odma_qkv_prep {
 } odma_qkv_prep;
 /* q: device, [n_new_total, q_heads, D]; k_new, v_new: device, [n_new_total, kv_heads, D], in the pool's io
  * type, 16-byte aligned, heads of a token packed, tokens a stride apart.  q_out: device, packed
- * [n_new_total, q_heads, D], ready for odma_decode_attention; it may be q itself when q is packed, and
- * must not overlap the inputs otherwise.  tables: host- or device-built.  Rows of q_out that belong to
- * no request (or a refused one) are left as they were.  head_dim a multiple of 8, at most 256. */
+ * [n_new_total, q_heads, D], ready for odma_decode_attention; it may be q itself when q is packed (or one
+ * token), and must not overlap the inputs otherwise (ODMA_ERR_INVALID).  tables: host- or device-built.
+ * Rows of q_out that belong to no request (or a refused one) are left as they were.  head_dim a multiple
+ * of 8, at most 256. */
 int32_t odma_append_qkv(odma_pool* pool, int32_t layer, const odma_tables* tables, const void* q,
                         const void* k_new, const void* v_new, void* q_out, int32_t q_heads,
                         const odma_qkv_prep* prep, void* stream);

@@ -307,6 +307,14 @@ int32_t check_tables(const odma_pool* pool, const odma_tables* t) {
     return ODMA_OK;
 }
 
+// Does one of `rows` runs of `row` bytes, `stride` bytes apart from `first`, meet [out, out + bytes)?
+bool rows_meet(const void* first, int64_t row, int64_t stride, int64_t rows, const void* out, int64_t bytes) {
+    if (!first || row < 1) return false;
+    const int64_t d = static_cast<int64_t>(reinterpret_cast<uintptr_t>(out) - reinterpret_cast<uintptr_t>(first));
+    const int64_t t = d < row ? 0 : (d - row) / stride + 1;      // the first run that ends behind `out`
+    return t < rows && t * stride < d + bytes;
+}
+
 // The table is written by a kernel (odma_build_tables_device); its counts in the descriptor are bounds.
 bool built_on_device(const odma_tables* t) { return t->reserved != 0; }
 
@@ -847,6 +855,16 @@ int32_t odma_append_qkv(odma_pool* pool, int32_t layer, const odma_tables* table
     if (!q || !k_new || !v_new || !q_out || !aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(q_out) ||
         !aligned16(prep->q_norm) || !aligned16(prep->k_norm) || (reinterpret_cast<uintptr_t>(prep->inv_freq) & 3u) != 0 ||
         (reinterpret_cast<uintptr_t>(prep->positions) & 3u) != 0)
+        return ODMA_ERR_INVALID;
+    // q_out over rows that another block has still to read: only q itself, row on row
+    const int64_t es = pool->io_bytes, tokens = tables->n_new_total, out_bytes = tokens * packed_q * es;
+    const bool in_place = q_out == q && (p.q_stride == packed_q || tokens == 1);
+    if ((!in_place && rows_meet(q, packed_q * es, p.q_stride * es, tokens, q_out, out_bytes)) ||
+        rows_meet(k_new, packed_kv * es, p.k_stride * es, tokens, q_out, out_bytes) ||
+        rows_meet(v_new, packed_kv * es, p.v_stride * es, tokens, q_out, out_bytes) ||
+        rows_meet(prep->q_norm, D * es, D * es, 1, q_out, out_bytes) || rows_meet(prep->k_norm, D * es, D * es, 1, q_out, out_bytes) ||
+        (pairs > 0 && (rows_meet(prep->inv_freq, pairs * 4ll, pairs * 4ll, 1, q_out, out_bytes) ||
+                       rows_meet(prep->positions, tokens * 4, p.pos_stride * 4, prep->n_axes, q_out, out_bytes))))
         return ODMA_ERR_INVALID;
     const int32_t* tab = static_cast<const int32_t*>(tables->d_table);
     p.base = tab + tables->off_base;

@@ -85,3 +85,49 @@ def test_a_timeout_does_not_hide_a_refusal(refused_first):
     if not refused_first:
         refuse(s.stream)
     assert [s.pool.check_status(s.stream) for _ in range(3)] == [odma.ERR_TIMEOUT, odma.ERR_OVERFLOW, odma.OK]
+
+
+# ---- append_qkv: where the queries may go ---------------------------------------------------------------
+
+@pytest.mark.parametrize("kind,d", [("bf16", 64), ("f32", 32)])
+def test_append_qkv_refuses_queries_over_rows_still_to_be_read(kind, d):
+    """q_out is packed.  Over strided queries (or any other input) it lies on rows of tokens that other blocks still read."""
+    s = SlabPool([32, 32, 32], [4, 9, 2], 1, 2, d, kind)
+    odma, t = s.odma, s.tables([0, 1, 2])
+    es, heads = s.mem.element_size(), 4
+    row, kv, n = heads * d, 2 * d, 3
+    x = torch.zeros(1 << 14, dtype=s.io, device="cuda")
+    b = x.data_ptr() + 4096
+    freq, pos = torch.ones(d // 2, device="cuda"), torch.zeros(64, dtype=torch.int32, device="cuda")
+    far = x.data_ptr() + (x.numel() - n * row) * es              # behind everything else
+
+    def rc(q, k, v, out, tables=t, **kw):
+        p = odma.QkvPrep(**{"rot_dim": d, "inv_freq": freq.data_ptr(), **kw})
+        return odma._lib.odma_append_qkv(s.pool._h, 0, ctypes.byref(tables), q, k, v, out, heads, ctypes.byref(p), s.stream)
+
+    # one projection's output: [n, heads + 4 KV rows, d]
+    wide = row + 2 * kv
+    strides = {"q_stride": wide, "k_stride": wide, "v_stride": wide}
+    fused = (b, b + row * es, b + (row + kv) * es)
+    before = s.mem.clone()
+    for out in (b, b + 16, b + row * es, b + (n - 1) * wide * es, b - (n * row - 8) * es, b + (n * wide - 8) * es):
+        assert rc(*fused, out, **strides) == odma.ERR_INVALID, out - b
+    # packed inputs
+    packed = (b, b + n * row * es, b + n * (row + kv) * es)
+    for out in (b + 16, b - 16, b + row * es, packed[1], packed[2], packed[2] + n * kv * es - 16):
+        assert rc(*packed, out) == odma.ERR_INVALID, out - b
+    for kw in ({"q_norm": far}, {"k_norm": far + (n * row - d) * es}, {"inv_freq": far + 16}, {"positions": far}):
+        assert rc(*packed, far, **kw) == odma.ERR_INVALID, kw
+    torch.cuda.synchronize()
+    assert torch.equal(s.mem.view(torch.uint8), before.view(torch.uint8)) and not x.any()
+    # side by side, in place, and in the gaps between strided rows
+    assert rc(*fused, b - n * row * es, **strides) == odma.OK
+    assert rc(*fused, b + n * wide * es, **strides) == odma.OK
+    assert rc(*packed, b) == odma.OK
+    assert rc(*packed, b - n * row * es) == odma.OK
+    gap = wide + n * row
+    assert rc(*fused, b + wide * es, q_stride=gap, k_stride=gap, v_stride=gap) == odma.OK
+    one = SlabPool([32], [4], 1, 2, d, kind)
+    p = odma.QkvPrep(rot_dim=d, inv_freq=freq.data_ptr(), positions=pos.data_ptr(), **strides)
+    assert odma._lib.odma_append_qkv(one.pool._h, 0, ctypes.byref(one.tables([0])), *fused, b, heads, ctypes.byref(p), one.stream) == odma.OK
+    assert s.sync() == 0 and one.sync() == 0
