@@ -126,26 +126,36 @@ typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t,
                                   CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion,
                                   CUtensorMapFloatOOBfill);
 
-// Four views of a [rows x head_dim] row array of 2-byte (bf16) or 1-byte (E4M3) elements: boxes of
-// 16, 32, 48 and 64 rows by 128 bytes (the widest inner extent the 128-byte swizzle allows).
-int32_t make_tensor_maps(void* base, int64_t rows, int32_t head_dim, int32_t elem_bytes, TensorMaps* out) {
-    void* fn = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q) != cudaSuccess ||
-        q != cudaDriverEntryPointSuccess || !fn)
-        return ODMA_ERR_CUDA;
-    auto encode = reinterpret_cast<EncodeTiledFn>(fn);
+// The driver's encoder, looked up once.
+EncodeTiledFn tensor_map_encoder() {
+    static const EncodeTiledFn encode = []() -> EncodeTiledFn {
+        void* fn = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess)
+            return nullptr;
+        return reinterpret_cast<EncodeTiledFn>(fn);
+    }();
+    return encode;
+}
+
+// View of a [rows x head_dim] row array of 2-byte (bf16) or 1-byte (E4M3) elements by boxes of `box_rows` rows by
+// 128 bytes (the widest inner extent the 128-byte swizzle allows).
+bool make_tensor_map(void* base, int64_t rows, int32_t head_dim, int32_t elem_bytes, int32_t box_rows, CUtensorMap* out) {
+    const EncodeTiledFn encode = tensor_map_encoder();
+    if (!encode) return false;
     const cuuint64_t gdim[2] = {static_cast<cuuint64_t>(head_dim), static_cast<cuuint64_t>(rows)};
     const cuuint64_t gstride[1] = {static_cast<cuuint64_t>(head_dim) * elem_bytes};
     const cuuint32_t estride[2] = {1, 1};
     const CUtensorMapDataType type = elem_bytes == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
-    for (int k = 0; k < 4; ++k) {
-        const cuuint32_t box[2] = {static_cast<cuuint32_t>(128 / elem_bytes), static_cast<cuuint32_t>(16 * (k + 1))};
-        if (encode(&out->box[k], type, 2, base, gdim, gstride, box, estride,
-                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-            return ODMA_ERR_CUDA;
-    }
+    const cuuint32_t box[2] = {static_cast<cuuint32_t>(128 / elem_bytes), static_cast<cuuint32_t>(box_rows)};
+    return encode(out, type, 2, base, gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Four views: boxes of 16, 32, 48 and 64 rows.
+int32_t make_tensor_maps(void* base, int64_t rows, int32_t head_dim, int32_t elem_bytes, TensorMaps* out) {
+    for (int k = 0; k < 4; ++k)
+        if (!make_tensor_map(base, rows, head_dim, elem_bytes, 16 * (k + 1), &out->box[k])) return ODMA_ERR_CUDA;
     return ODMA_OK;
 }
 
@@ -1113,6 +1123,11 @@ int32_t odma_decode_attention_prefix(odma_pool* pool, int32_t layer, const void*
     fill_decode_params(pool, layer, q, q_heads, tables, out, lse, &p);
     p.counters = nullptr;
     p.partial_only = 1;
+    // whatever may refuse the call comes before its first launch
+    const bool tensor_own = uses_tc(pool, q_heads), fp8 = pool->dtype == ODMA_DTYPE_FP8_E4M3;
+    if (tensor_own && p.stages < 2) return ODMA_ERR_INVALID;
+    CUtensorMap widened;                         // 8-bit pools: the prefix as bf16, in the workspace
+    if (fp8 && splits > 0 && !make_tensor_map(workspace, 2ll * pool->kv_heads * w.pad, D, 2, 64, &widened)) return ODMA_ERR_CUDA;
 
     pool->decode_was_last = false;               // other kernels of this call lie between decode launches
     pool->last_fused_tensor = false;
@@ -1142,8 +1157,7 @@ int32_t odma_decode_attention_prefix(odma_pool* pool, int32_t layer, const void*
         pp.k_row0 = static_cast<int32_t>(k_row0);
         pp.v_row0 = static_cast<int32_t>(k_row0 + pool->rows_per_array);
         ProfScope ps(pool, ODMA_K_DECODE, s);
-        TensorMaps ws_maps{};
-        if (pool->dtype == ODMA_DTYPE_FP8_E4M3) {
+        if (fp8) {
             if (launch_dequant_prefix(k, v, pr->cap, prefix_len, w.pad, pool->kv_heads, D, workspace, s) != cudaSuccess)
                 return ODMA_ERR_CUDA;
             pp.k = workspace;
@@ -1151,17 +1165,14 @@ int32_t odma_decode_attention_prefix(odma_pool* pool, int32_t layer, const void*
             pp.head_rows = w.pad;
             pp.k_row0 = 0;
             pp.v_row0 = pool->kv_heads * w.pad;
-            if (make_tensor_maps(workspace, 2ll * pool->kv_heads * w.pad, D, 2, &ws_maps) != ODMA_OK) return ODMA_ERR_CUDA;
         }
-        const TensorMaps& maps = pool->dtype == ODMA_DTYPE_FP8_E4M3 ? ws_maps : pool->maps;
-        const cudaError_t e = tensor ? launch_prefix_umma(maps.box[3], pp, pool->dtype == ODMA_DTYPE_FP8_E4M3, s) : launch_prefix(pp, fp32, s);
+        const cudaError_t e = tensor ? launch_prefix_umma(fp8 ? widened : pool->maps.box[3], pp, fp8, s) : launch_prefix(pp, fp32, s);
         if (e != cudaSuccess) return ODMA_ERR_CUDA;
     }
     {
         ProfScope ps(pool, ODMA_K_DECODE, s);
         cudaError_t e;
-        if (uses_tc(pool, q_heads)) {
-            if (p.stages < 2) return ODMA_ERR_INVALID;
+        if (tensor_own) {
             // Behind the prefix's kernel the launch need not wait: the tables, queries and slab rows were complete before
             // that kernel began (it waits for all work ahead of it), and it writes only the workspace.  So the tcgen05
             // kernel runs as a chained launch, or the other one asks for its first rows early.

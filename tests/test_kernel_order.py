@@ -22,3 +22,15 @@ def test_dependents_are_let_go_behind_the_allocation(name):
         code = re.sub(r"//[^\n]*", "", f.read())
     alloc, go = code.index("tcgen05.alloc"), [m.start() for m in re.finditer(r"griddepcontrol\.launch_dependents", code)]
     assert go and alloc < min(go)
+
+
+def test_a_prefix_call_is_refused_before_its_first_launch():
+    """Everything that can refuse the call (the tensor map of the widened prefix among it) stands before the kernel that
+    the call launches first; behind it only a launch can fail."""
+    with open(os.path.join(CSRC, "api.cu")) as f:
+        code = re.sub(r"//[^\n]*", "", f.read())
+    body = code[code.index("int32_t odma_decode_attention_prefix("):]
+    body = body[:body.index("\n}\n")]
+    launched = body[body.index("launch_"):]
+    assert "ODMA_ERR_INVALID" not in launched and "make_tensor_map" not in launched
+    assert "make_tensor_map" in body
