@@ -70,6 +70,7 @@ struct odma_pool {
     size_t part_o_floats = 0, part_ml_floats = 0;      // of ONE set
     int32_t last_lo = -1, last_hi = -1;                // layers the last decode launch covered
     int64_t slots_max = 0;
+    int32_t prefix_blocks = 1;           // blocks of the shared prefix's kernel that an SM holds
     int64_t table_words_max = 0;
     bool has_maps = false;
     TensorMaps maps{};
@@ -484,6 +485,8 @@ int32_t odma_pool_create(void* dev_base, uint64_t bytes, int32_t layers, int32_t
         if (cfg.plan_ctas == 0) p->plan_ctas = sms;
     }
     p->slots_max = static_cast<int64_t>(cfg.max_batch) * kv_heads + p->plan_ctas;
+    if (dtype == ODMA_DTYPE_F32 || !tc_supported(head_dim, 1))
+        p->prefix_blocks = prefix_generic_blocks(dtype == ODMA_DTYPE_F32, head_dim, dev_base != nullptr);
     p->table_words_max = plan_table_words(cfg.max_batch, kv_heads, p->plan_ctas);
     if (dev_base) {
         const size_t po = static_cast<size_t>(p->slots_max) * cfg.max_group * head_dim * 4;
@@ -1077,7 +1080,8 @@ bool prefix_on_tensor(const odma_pool* pool) { return pool->dtype != ODMA_DTYPE_
 
 PrefixSplit prefix_split_of(const odma_pool* pool, int32_t q_heads, int32_t n, int32_t len) {
     if (len < 1) return PrefixSplit{0, 0};
-    return prefix_split(n * (q_heads / pool->kv_heads), n * q_heads, pool->kv_heads, len, pool->plan_ctas, prefix_on_tensor(pool));
+    return prefix_split(n * (q_heads / pool->kv_heads), n * q_heads, pool->kv_heads, len, pool->plan_ctas,
+                        pool->prefix_blocks, prefix_on_tensor(pool));
 }
 
 bool prefix_shape_ok(const odma_pool* pool, int32_t q_heads, int32_t n, int32_t len) {

@@ -208,7 +208,8 @@ struct PrefixSplit {
     int32_t splits;             // partial results per query row
     int32_t in_turn;            // see PrefixParams
 };
-PrefixSplit prefix_split(int32_t rows, int32_t q_rows, int32_t kv_heads, int32_t len, int32_t sms, bool tensor);
+PrefixSplit prefix_split(int32_t rows, int32_t q_rows, int32_t kv_heads, int32_t len, int32_t sms, int32_t blocks_per_sm, bool tensor);
+int32_t prefix_generic_blocks(bool fp32, int32_t head_dim, bool ask);
 cudaError_t launch_prefix(const PrefixParams& p, bool fp32, cudaStream_t stream);
 // `behind_dequant`: the kernel ahead is launch_dequant_prefix, itself launched behind everything else; otherwise this one
 // waits for all work ahead of it.  Either way the kernel behind it may begin at once (programmatic launch).

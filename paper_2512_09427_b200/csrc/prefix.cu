@@ -350,12 +350,12 @@ cudaError_t launch_generic_t(const PrefixParams& p, cudaStream_t s) {
 // partial results cost), by measured figures in ns.  Tensor cores (one block per SM): 6,500 for a block's set-up,
 // queries and hand-over, and per step of 64 keys 1,100 with two row tiles, 900 with one; when one row tile's steps
 // go to the two lanes in turn, 7,500 and 750 (it pays from four tiles of 128 keys per block on: 3 requests, 777
-// keys, 2 blocks: 14.1 us against 14.4; 7 blocks: 12.4 against 11.0).  Plain ALUs (8 rows, four blocks per SM): 3,000 and 5,000 per tile
-// of 128 keys.  A row's partial result costs its write and its read in the merge, 0.2.
-PrefixSplit prefix_split(int32_t rows, int32_t q_rows, int32_t kv_heads, int32_t len, int32_t sms, bool tensor) {
+// keys, 2 blocks: 14.1 us against 14.4; 7 blocks: 12.4 against 11.0).  Plain ALUs (8 rows, blocks_per_sm of them on an
+// SM): 3,000 and 5,000 per tile of 128 keys.  A row's partial result costs its write and its read in the merge, 0.2.
+PrefixSplit prefix_split(int32_t rows, int32_t q_rows, int32_t kv_heads, int32_t len, int32_t sms, int32_t blocks_per_sm, bool tensor) {
     const int64_t tiles = (len + kPrefixTile - 1) / kPrefixTile;
     const int64_t blocks = kv_heads * static_cast<int64_t>(tensor ? (rows + 255) / 256 : (rows + kRows - 1) / kRows);
-    const int64_t room = tensor ? sms : 4ll * sms;
+    const int64_t room = static_cast<int64_t>(blocks_per_sm) * sms;
     PrefixSplit best{1, 0};
     int64_t least = INT64_MAX;
     for (int32_t s = 1; s <= std::min<int64_t>(tiles, kMaxPrefixSplits); ++s) {
@@ -372,6 +372,22 @@ PrefixSplit prefix_split(int32_t rows, int32_t q_rows, int32_t kv_heads, int32_t
         }
     }
     return best;
+}
+
+// Blocks of prefix_generic_kernel that an SM holds: the runtime's answer, or what it is on sm_100a where there is no device
+// to ask (122 to 126 registers at head_dim 32, 150 and 156 at 64 and 128).
+int32_t prefix_generic_blocks(bool fp32, int32_t head_dim, bool ask) {
+    int blocks = 0;
+    cudaError_t e = cudaErrorNotSupported;
+    if (ask) {
+        const void* kernel = !fp32            ? reinterpret_cast<const void*>(&prefix_generic_kernel<__nv_bfloat16, 1>)
+                             : head_dim == 32 ? reinterpret_cast<const void*>(&prefix_generic_kernel<float, 1>)
+                             : head_dim == 64 ? reinterpret_cast<const void*>(&prefix_generic_kernel<float, 2>)
+                                              : reinterpret_cast<const void*>(&prefix_generic_kernel<float, 4>);
+        e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&blocks, kernel, kWarps * 32, 0);
+        if (e != cudaSuccess) cudaGetLastError();      // not the next launch's
+    }
+    return e == cudaSuccess && blocks > 0 ? blocks : head_dim == 32 ? 4 : 3;
 }
 
 cudaError_t launch_prefix(const PrefixParams& p, bool fp32, cudaStream_t stream) {
