@@ -1,12 +1,12 @@
 """Calls around slab attention next to one another: status words, streams, splits of a prefix and operands that overlap."""
 import ctypes
-import random
 
 import pytest
 import torch
 
 import operator_refs as ref
 from operator_refs import SlabPool
+from test_gpu_operators import device_plan, run_prefix
 
 pytestmark = pytest.mark.gpu
 
@@ -163,3 +163,26 @@ def test_a_request_without_new_rows_is_not_refused_behind_rows_that_do_not_fit(n
     want, _, bound, _ = s.reference(0, q[2:3], [2], [20])
     ref.within(out[2:3], want, bound, "out")
     assert (out[[r for r in range(5) if not after[r]]] == 7.0).all()
+
+
+# ---- the late read-out on plans of the device ------------------------------------------------------------
+
+@pytest.mark.parametrize("d,q_heads", [(128, 14), (64, 24)])
+@pytest.mark.parametrize("lens", [[1], [0, 5, 0], [700, 64, 1, 65, 0, 333], [40] * 33])
+def test_late_readout_from_device_tables_and_behind_a_prefix(d, q_heads, lens):
+    """Shares without an item, many items per share, and every item left as a partial result."""
+    odma = ref.lib()
+    caps = [(x + 31) // 16 * 16 for x in lens] + [272]
+    s = SlabPool(caps, lens + [260], 1, 2, d, "bf16", ctas=6, decode_kernel=odma.DECODE_TCGEN05, readout=odma.READOUT_LATE)
+    n = len(lens)
+    reqs = list(range(n))
+    t = device_plan(s, reqs, [0] * n)
+    q = s.randn(n, q_heads, d)
+    out = torch.full_like(q, 7.0)
+    s.pool.decode_attention(0, q.data_ptr(), q_heads, t, out.data_ptr(), 0, s.stream)
+    assert s.sync() == odma.OK
+    want, _, bound, _ = s.reference(0, q, reqs, lens)
+    full = torch.tensor([x > 0 for x in lens])
+    ref.within(out[full.cuda()], want[full], bound[full], "out")
+    assert (out[~full.cuda()] == 7.0).all()
+    run_prefix(s, reqs, lens, n, 260, q_heads, t, repeat=2)
