@@ -220,8 +220,9 @@ int32_t odma_observe(odma_pool* pool, const int32_t* lengths, int32_t n);
  * host, [layers] fp32, finite and > 0.  A stored code c of layer l stands for value(c) *
  * scale[l]; an append stores the code nearest (ties to even, saturating at +-448) to
  * fp32(x) * (1.0f / scale[l]), product and reciprocal taken in fp32.  Default 1 for every
- * layer.  Takes effect for launches issued after the call; rows already stored keep their
- * codes.  ODMA_ERR_INVALID for another pool type or a bad scale. */
+ * layer.  Takes effect for launches issued after the call (a captured graph keeps the scales of
+ * its capture: capture again); rows already stored keep their codes.  ODMA_ERR_INVALID for
+ * another pool type or a bad scale. */
 int32_t odma_set_kv_scales(odma_pool* pool, const float* k_scale, const float* v_scale);
 
 /* ---- bucket boundaries (Section III-C, Eq. 2) ------------------------------------------
@@ -375,7 +376,7 @@ typedef struct odma_qkv_prep {
  * [n_new_total, q_heads, D], ready for odma_decode_attention; it may be q itself when q is packed (or one
  * token), and must not overlap the inputs otherwise (ODMA_ERR_INVALID).  tables: host- or device-built.
  * Rows of q_out that belong to no request (or a refused one) are left as they were.  head_dim a multiple
- * of 8, at most 256. */
+ * of 8, at most 256.  A captured call keeps an 8-bit pool's scales (odma_set_kv_scales). */
 int32_t odma_append_qkv(odma_pool* pool, int32_t layer, const odma_tables* tables, const void* q,
                         const void* k_new, const void* v_new, void* q_out, int32_t q_heads,
                         const odma_qkv_prep* prep, void* stream);
@@ -395,7 +396,8 @@ int32_t odma_decode_attention(odma_pool* pool, int32_t layer, const void* q, int
  * the first prefix_len tokens of that slab,
  *   out[i][h] = softmax_j(q[i][h] . [K_P ; K_i][j] / sqrt(head_dim)) [V_P ; V_i],   lse likewise.
  * The prefix's part is computed for the whole batch at once, its keys and values read once per 256
- * query rows of a KV head instead of once per request.  prefix_len may be 0 .. the prefix's committed
+ * query rows of a KV head (16- and 8-bit slabs of head_dim 64 and 128; once per 8 rows in fp32 slabs
+ * and at head_dim 32) instead of once per request.  prefix_len may be 0 .. the prefix's committed
  * length (ODMA_ERR_OVERFLOW beyond); a request of a device-built table without a token of its own
  * gets the prefix alone (with prefix_len 0: zeros and an lse of -inf).  Arguments otherwise as for
  * odma_decode_attention; head_dim 32, 64 or 128.
@@ -403,8 +405,8 @@ int32_t odma_decode_attention(odma_pool* pool, int32_t layer, const void* q, int
  * 8-bit pool, the prefix as bf16).  odma_prefix_workspace_bytes gives the size for n requests at the
  * best number of splits (0 for a bad shape); with less, down to one split, the call uses fewer.
  * Calls of one pool are ordered, as everywhere, and may share a workspace; calls of two pools that overlap on
- * the GPU need one each.  A captured call keeps the place of the
- * prefix's slab and prefix_len: capture again when that request has moved or been freed. */
+ * the GPU need one each.  A captured call keeps the place of the prefix's slab, prefix_len and an 8-bit
+ * pool's scales: capture again when that request has moved or been freed, or the scales have changed. */
 uint64_t odma_prefix_workspace_bytes(const odma_pool* pool, int32_t q_heads, int32_t n, int32_t prefix_len);
 int32_t odma_decode_attention_prefix(odma_pool* pool, int32_t layer, const void* q, int32_t q_heads,
                                      uint64_t prefix_req, int32_t prefix_len, const odma_tables* tables,
