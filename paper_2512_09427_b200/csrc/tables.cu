@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(kThreads) __cluster_dims__(kCluster, 1, 1) bui
         const bool counted = add[k] >= 0 && add[k] <= p.n_new_total;
         const bool ok = counted && base[k] >= 0 && (base[k] & 15) == 0 && cap[k] >= 0 &&
                         static_cast<int64_t>(base[k]) + cap[k] <= p.tokens && len[k] >= 0 &&
-                        static_cast<int64_t>(len[k]) + add[k] <= cap[k] && (add[k] == 0 || at + add[k] <= p.n_new_total);
+                        static_cast<int64_t>(len[k]) + add[k] <= cap[k] && at + add[k] <= p.n_new_total;
         cu[i] = static_cast<int32_t>(min(at, static_cast<int64_t>(p.n_new_total)));
         if (counted) at += add[k];
         if (i == n - 1) cu[n] = static_cast<int32_t>(min(at, static_cast<int64_t>(p.n_new_total)));
