@@ -305,8 +305,9 @@ int32_t odma_build_tables(odma_pool* pool, const uint64_t* reqs, const int32_t* 
  * ceil(cost / n_ctas)); a cut closer than 3 tiles to an end of its stream moves to that end, a stream
  * shorter than 6 tiles is not cut.
  * A request that breaks base % 16 = 0, 0 <= base, base + cap <= T, 0 <= len, 0 <= n_new, len + n_new <=
- * cap, or whose rows pass n_new_total, is refused: base, cap and len words 0, no item, its rows of the
- * slot map -1, its length not advanced, nothing appended for it; odma_check_status then returns
+ * cap, or for which its new rows and those of the requests before it pass n_new_total (from the first such
+ * request on, all behind it too, with new rows or without), is refused: base, cap and len words 0, no
+ * item, its rows of the slot map -1, its length not advanced, nothing appended for it; odma_check_status then returns
  * ODMA_ERR_OVERFLOW.  (n_new outside [0, n_new_total] counts as 0 rows.)  That two slabs do not
  * overlap is not checked.
  * The host's lengths do not follow: commit them with odma_commit_step before the next call that uses

@@ -133,6 +133,40 @@ def test_append_qkv_refuses_queries_over_rows_still_to_be_read(kind, d):
     assert s.sync() == 0 and one.sync() == 0
 
 
+# ---- tables ------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("new,after,cu,positions", [
+    # five rows of four: counts as none, and request 3 has the last row
+    ([3, 5, 0, 1, 0], [13, 0, 20, 8, 0], [0, 3, 3, 3, 4, 4], [10, 11, 12, 7]),
+    # rows 3 and 4 of four: request 1 and whatever is behind it, with rows or without
+    ([3, 2, 0, 1, 0], [13, 0, 0, 0, 0], [0, 3, 4, 4, 4, 4], [10, 11, 12, -1])])
+def test_rows_that_do_not_fit_and_the_requests_behind_them(new, after, cu, positions):
+    odma = ref.lib()
+    lens = [10, 5, 20, 7, 0]
+    s = SlabPool([32, 32, 32, 32, 16], lens, 1, 2, 64, "bf16")
+    slabs = torch.empty(5, 2, dtype=torch.int32, device="cuda")
+    length, nxt, slots, pos = torch.empty(5, dtype=torch.int32, device="cuda"), dev([-9] * 5), dev([-9] * 4), dev([-9] * 4)
+    s.pool.slab_table(range(5), slabs.data_ptr(), length.data_ptr(), s.stream)
+    d_new = dev(new)
+    t = s.pool.build_tables_device(slabs.data_ptr(), length.data_ptr(), 5, 4, s.table.data_ptr(), s.table.numel(), d_new.data_ptr(),
+                                   nxt.data_ptr(), slots.data_ptr(), pos.data_ptr(), s.stream)
+    assert s.sync() == odma.ERR_OVERFLOW
+    words = s.table.view(torch.int32).tolist()
+    assert words[t.off_len:t.off_len + 5] == after and words[t.off_cu_new:t.off_cu_new + 6] == cu
+    assert nxt.tolist() == [a or x for a, x in zip(after, lens)] and pos.tolist() == positions
+    owner = [0, 0, 0, 3]
+    assert slots.tolist() == [s.base[r] * 2 + p if p >= 0 else -1 for r, p in zip(owner, positions)]
+    q = s.randn(5, 4, 64)
+    out = torch.full_like(q, 7.0)
+    s.pool.decode_attention(0, q.data_ptr(), 4, t, out.data_ptr(), 0, s.stream)
+    assert s.sync() == odma.OK
+    for r in (0, 2, 3):
+        if after[r] == lens[r]:                                   # (rows of this step's tokens have not been written)
+            want, _, bound, _ = s.reference(0, q[r:r + 1], [r], [lens[r]])
+            ref.within(out[r:r + 1], want, bound, "out")
+    assert (out[[r for r in range(5) if not after[r]]] == 7.0).all()
+
+
 # ---- the late read-out on plans of the device ------------------------------------------------------------
 
 @pytest.mark.parametrize("d,q_heads", [(128, 14), (64, 24)])
