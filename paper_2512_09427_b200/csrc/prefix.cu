@@ -11,7 +11,8 @@
 //
 //  prefix_umma_kernel      tcgen05 tensor cores (prefix_umma.cu): 16- and 8-bit slabs, head_dim 64 and 128
 //  prefix_generic_kernel   plain ALUs, fp32 arithmetic: fp32 slabs, head_dim 32.  Eight rows per block share every
-//                          key; small calls are a chain of latencies (4 requests, 1,000 keys, head_dim 64: 7.9 us)
+//                          key; small calls are a chain of latencies (4 requests, 1,000 keys, head_dim 64: the whole
+//                          call 16.6 us, this kernel alone and cold 10.6)
 //  dequant_prefix_kernel   8-bit slabs: the prefix's codes as bf16 (exact: a code has 4 significant
 //                          bits); the scales stay outside, in the score factor and in the merge
 //  merge_prefix_kernel     own pieces and prefix splits to out and lse
@@ -204,7 +205,7 @@ __global__ void __launch_bounds__(kWarps * 32) prefix_generic_kernel(const Prefi
 // Codes [kv_heads][len][D] of K and V (rows of a head head_rows apart) to bf16 [2][kv_heads][pad][D].  A thread takes
 // kDequant vectors of 16 codes, all loads before the first store, and the prefix's kernel sets itself up beside this
 // one, which its set-up needs nothing of (47 requests, 5,001 keys, the whole call: 30.4 us with one vector and the
-// kernels in a row, 29.2 so; 64 requests, 32,768 keys: 75.5 and 73.6).
+// kernels in a row, 29.1 to 30.5 so; 64 requests, 32,768 keys: 75.5 and 73.6).
 constexpr int kDequant = 4;
 __global__ void __launch_bounds__(256) dequant_prefix_kernel(const uint8_t* k, const uint8_t* v, int64_t head_rows, int len,
                                                              int pad, int kv_heads, int D, __nv_bfloat16* out) {

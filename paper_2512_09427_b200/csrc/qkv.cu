@@ -11,10 +11,11 @@
 // in fp32: a position of 10^6 times an fp32 frequency keeps no digits of the turn in 32 bits.
 //
 // Each input element is read once and each output element written once: a chunk of 8,192 tokens of the
-// 28 + 4 + 4-head layer moves 151 MB, 23.4 us at the measured copy rate; the kernel takes 35.5 us (4.3 TB/s).
-// Beside the memory it is instruction issue that bounds it (59 % of the issue slots): a row of 128
-// elements over 16 lanes of eight took 245 instructions per warp and 43 us, over 8 lanes of sixteen, with a
-// token's addresses, turns and weights in registers and packed arithmetic, 35.5.  One token, or 256: 3.0
+// 28 + 4 + 4-head layer moves 151 MB, 23.4 us at the measured copy rate; the kernel takes 35.8 us (4.2 TB/s).
+// Neither the memory nor instruction issue (59 % of the slots) is full: a block's way to its first store
+// (owner, length, angle, barrier) is the rest.  A row of 128 elements over 16 lanes of eight took 245
+// instructions per warp and 43 us, over 8 lanes of sixteen, with a token's addresses, turns and weights in
+// registers and packed arithmetic, 35.8.  Into an 8-bit pool (143 MB, 22.1 us) it takes 34.3.  One token, or 256: 3.0
 // and 3.8 us, a chain of latencies (owner, position, angle, row).  A token's rot_dim / 2 sines and cosines are
 // computed once, into shared memory, under the latency of the first row loads, and serve all its heads.
 // A row is held by D / 16 (D / 8) lanes, laid out so that both elements of a pair sit in the same lane
