@@ -862,6 +862,9 @@ int32_t odma_append_qkv(odma_pool* pool, int32_t layer, const odma_tables* table
     p.pos_stride = prep->pos_stride ? prep->pos_stride : tables->n_new_total;
     if (p.q_stride < packed_q || p.k_stride < packed_kv || p.v_stride < packed_kv || p.pos_stride < tables->n_new_total)
         return ODMA_ERR_INVALID;
+    constexpr int64_t kMaxStride = int64_t(1) << 46;             // beyond any memory; bytes and offsets stay within 64 bits
+    if (p.q_stride > kMaxStride || p.k_stride > kMaxStride || p.v_stride > kMaxStride || p.pos_stride > kMaxStride)
+        return ODMA_ERR_INVALID;
     if (p.q_stride * pool->io_bytes % 16 != 0 || p.k_stride * pool->io_bytes % 16 != 0 || p.v_stride * pool->io_bytes % 16 != 0)
         return ODMA_ERR_INVALID;
     if (tables->n_new_total == 0) return ODMA_OK;

@@ -26,12 +26,12 @@
 //
 // What bounds it: the tensor pipe.  32,768 keys and 7,168 rows (120 GFLOP): 108 us for this kernel alone, 1.1 PFLOP/s
 // (0.66 of the measured burst rate), the whole call 137 us in a burst and 146 to 152 sustained (the GPU then sits at its
-// power limit, 985 W); 1,570 cycles per step of 64 keys and 256 rows.  An instruction takes 64 cycles, the first product's, 64 keys wide, no less than one of 128 keys
-// (2 x (8 + 4) x 64 = 1,536); with a quarter of the first product's instructions the call took 124 us instead of
-// 140, of the second's 130, without the exponentials 132, without loads 138.  Steps of 128 keys would halve the
-// first product's count and leave one S buffer per lane, whose chain of softmax and products is about as long.  A
-// block's set-up, queries and hand-over cost 6.5 us, of which the 128 KB of its partial results are 2.4: that is what
-// short prefixes pay for.
+// power limit, 985 W); 1,570 cycles per step of 64 keys and 256 rows.  An instruction takes 64 cycles, the first
+// product's, 64 keys wide, no less than one of 128 keys (2 x (8 + 4) x 64 = 1,536); with a quarter of the first
+// product's instructions the call took 124 us instead of 140, of the second's 130, without the exponentials 132,
+// without loads 138.  Steps of 128 keys would halve the first product's count and leave one S buffer per lane, whose
+// chain of softmax and products is about as long.  A block's set-up, queries and hand-over cost 6.5 us, of which the
+// 128 KB of its partial results are 2.4: that is what short prefixes pay for.
 #include "odma.h"
 #include "tcgen05.cuh"
 

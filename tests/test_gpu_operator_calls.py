@@ -132,6 +132,18 @@ def test_append_qkv_refuses_queries_over_rows_still_to_be_read(kind, d):
     assert odma._lib.odma_append_qkv(one.pool._h, 0, ctypes.byref(one.tables([0])), *fused, b, heads, ctypes.byref(p), one.stream) == odma.OK
     assert s.sync() == 0 and one.sync() == 0
 
+@pytest.mark.parametrize("which", ["q_stride", "k_stride", "v_stride", "pos_stride"])
+def test_append_qkv_refuses_strides_beyond_any_memory(which):
+    """Among them those whose bytes pass 64 bits."""
+    s = SlabPool([32, 32], [4, 9], 1, 2, 64, "f32")
+    odma, t = s.odma, s.tables([0, 1])
+    x = torch.zeros(1 << 13, dtype=torch.float32, device="cuda")
+    b = x.data_ptr()
+    for stride in ((1 << 46) + 4, 1 << 60, 1 << 62, (1 << 63) - 4):
+        p = odma.QkvPrep(rot_dim=64, inv_freq=b + 16384, positions=b + 20480, **{which: stride})
+        assert odma._lib.odma_append_qkv(s.pool._h, 0, ctypes.byref(t), b, b + 4096, b + 8192, b + 24576, 4, ctypes.byref(p), s.stream) == odma.ERR_INVALID
+    assert s.sync() == 0
+
 
 # ---- tables ------------------------------------------------------------------------------------------
 
