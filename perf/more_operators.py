@@ -341,7 +341,7 @@ def _plain_store(s):
             x = x.view(*x.shape[:-1], -1, group)                        # [tokens, heads, groups, group]
             top = x.abs().amax(-1)
             zero = top < TINY_GROUP
-            scale = top / TOP[fmt]
+            scale = top / (one * TOP[fmt])                              # a true division, not a product with 1 / TOP
             inv = torch.where(zero, 0.0, one / scale)[..., None]
             s["scales"][a] = torch.where(zero, 0.0, scale)
             y = (x * inv).flatten(-2).clamp_(-TOP[fmt], TOP[fmt])
