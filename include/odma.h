@@ -80,6 +80,9 @@ enum { ODMA_DTYPE_F32 = 0, ODMA_DTYPE_BF16 = 1, ODMA_DTYPE_FP8_E4M3 = 2 };
 enum { ODMA_DECODE_AUTO = 0, ODMA_DECODE_TCGEN05 = 1, ODMA_DECODE_MMA_SYNC = 2 };
 enum { ODMA_READOUT_AUTO = 0, ODMA_READOUT_LATE = 1, ODMA_READOUT_AT_ONCE = 2 };
 
+/* how odma_pack_kv holds an element (odma_kv_store.format) */
+enum { ODMA_STORE_RAW = 0, ODMA_STORE_E4M3 = 1, ODMA_STORE_INT8 = 2, ODMA_STORE_INT4 = 3 };
+
 /* kernels that odma_profile_read can report */
 enum { ODMA_K_APPEND = 0, ODMA_K_DECODE = 1, ODMA_K_COMBINE = 2, ODMA_K_MIGRATE = 3,
        ODMA_K_PROBE = 4, ODMA_K_COUNT = 5 };
@@ -256,6 +259,42 @@ int32_t odma_ensure_capacity(odma_pool* pool, uint64_t req, int32_t needed_len, 
  * (Section IV-C). */
 int32_t odma_free(odma_pool* pool, uint64_t req);
 
+/* ---- rows of slabs out of the pool and back, in fewer bits -----------------------------------
+ * For a request that has to give its slab up for a while (ODMA_ERR_NOMEM, preemption) or goes on in another pool
+ * (another layer range, another replica): its rows go to a dense store of the caller's, and from there into any
+ * slab of any pool with the same heads, without being computed again.  The store holds, for the 2 * n_layers
+ * arrays of the layer range (layer by layer, K then V), the tokens of the call in order:
+ *   codes   [2 * n_layers][tokens][kv_heads][row]   16-byte aligned; row: head_dim elements of the format
+ *   scales  [2 * n_layers][tokens][kv_heads][head_dim / group] fp32 (not read or written in the raw format)
+ * A group is `group` elements of a row, 16, 32, 64, 128 or 256 of them, a divisor of head_dim.  Formats:
+ *   ODMA_STORE_RAW   the pool's own elements, bit for bit (only back into a pool of the same type)
+ *   ODMA_STORE_E4M3  E4M3 codes, largest value 448         ODMA_STORE_INT8  signed bytes, largest 127
+ *   ODMA_STORE_INT4  signed 4-bit numbers, largest 7, two to a byte, the first in the low half
+ * Arithmetic is fp32: scale = max |x| / largest, code = the number of the format nearest to x * (1.0f / scale), ties to
+ * even; back, code * scale, rounded once to the pool's type.  x is the element's value (in an 8-bit pool fp32
+ * code * scale of the layer, and back as odma_set_kv_scales describes).  A group whose largest magnitude is below
+ * 2^-100 has scale 0 and reads back as zeros; one that holds an infinity or a NaN has scale NaN and reads back as NaN. */
+typedef struct odma_kv_store {
+    void* codes;
+    float* scales;
+    uint64_t codes_bytes;        /* room behind the pointers, at least what odma_kv_store_bytes says */
+    uint64_t scales_bytes;
+    int32_t format, group;       /* group: not read in the raw format */
+    int32_t layer, n_layers;     /* the layer range */
+} odma_kv_store;
+/* Bytes of codes and scales for `tokens` tokens of n_layers layers. */
+int32_t odma_kv_store_bytes(const odma_pool* pool, int32_t format, int32_t group, int32_t n_layers, int64_t tokens,
+                            uint64_t* codes_bytes, uint64_t* scales_bytes);
+/* odma_pack_kv: tokens [first[i], first[i] + count[i]) of request i, i < n, to the store (first NULL: 0 each; count NULL:
+ * up to the committed length, beyond which it is ODMA_ERR_OVERFLOW).  odma_unpack_kv: from the store into the slabs,
+ * whose capacity bounds them; the same token twice is ODMA_ERR_INVALID, lengths are not committed
+ * (odma_commit_step).  One launch per 128 requests and 32 layers, asynchronous on `stream`, ordered like an append;
+ * a captured call keeps the slabs' places and an 8-bit pool's scales.  The store must not lie in the pool. */
+int32_t odma_pack_kv(odma_pool* pool, const uint64_t* reqs, const int32_t* first, const int32_t* count, int32_t n,
+                     const odma_kv_store* store, void* stream);
+int32_t odma_unpack_kv(odma_pool* pool, const uint64_t* reqs, const int32_t* first, const int32_t* count, int32_t n,
+                       const odma_kv_store* store, void* stream);
+
 /* Host mirror of the lengths: after a step's kernels have been issued, add n_new[i] (NULL =
  * 1 each) tokens to each request's length.  ODMA_ERR_OVERFLOW if one would pass its slab
  * (nothing is changed then). */
@@ -337,6 +376,25 @@ int32_t odma_build_tables_device(odma_pool* pool, const int32_t* d_slabs, const 
  * L2 after the first; packing several tokens of a chunk into one tensor-core tile is not done. */
 int32_t odma_build_prefill_tables(odma_pool* pool, const uint64_t* reqs, const int32_t* n_new, int32_t n,
                                   void* d_table, uint64_t table_bytes, void* stream, odma_tables* out);
+
+/* The same attention for any number of new tokens per request, by tiles of query rows: the tokens of a request and the
+ * query heads of a KV head share every key, so a slab is read once per 256 rows (16- and 8-bit slabs of head_dim 64 and
+ * 128, on the tensor cores; once per 64 rows in fp32 slabs and at head_dim 32) and not once per token.  tables: the step's
+ * own descriptor (odma_build_tables with n_new, or odma_build_tables_device), the one its rows were appended with;
+ * q, out: device, [n_new_total, q_heads, head_dim] in the pool's io type, 16-byte aligned, not overlapping; lse: device
+ * fp32 [n_new_total, q_heads] or NULL.  With len[i] the tokens after the step and t the j-th of n_new[i] new ones,
+ *   out[t][h] = softmax_{k <= len[i] - n_new[i] + j}(q[t][h] . K_i[h div g][k] / sqrt(head_dim)) V_i[h div g].
+ * Softmax and accumulation are fp32; on the tensor cores the weights are rounded to bf16 for the second product.  Rows that
+ * belong to no request (or a refused one) are left as they were.  A value row that is not finite makes the
+ * tokens before it in the same block of 128 keys NaN too (0 times it is not 0); a key row does not.
+ * head_dim 32, 64 or 128, at most 64 query heads per KV head and 4,096 requests.
+ * workspace: device, 256-byte aligned, the caller's: partial results of tiles that are cut between blocks and, for an
+ * 8-bit pool, the batch's rows as bf16 (of a device-built table: as many as the pool holds).
+ * odma_prefill_workspace_bytes gives the size for a descriptor (0 for a bad shape); a larger one serves too.  Calls
+ * that overlap on the GPU need one each.  May be captured; a captured call keeps an 8-bit pool's scales. */
+uint64_t odma_prefill_workspace_bytes(const odma_pool* pool, int32_t q_heads, const odma_tables* tables);
+int32_t odma_prefill_attention(odma_pool* pool, int32_t layer, const void* q, int32_t q_heads, const odma_tables* tables,
+                               void* workspace, uint64_t workspace_bytes, void* out, float* lse, void* stream);
 
 /* ---- KV append (the per-step growth of each request's cache, Section II-A) --------------
  * Writes the step's new K and V rows of `layer` behind each request's existing tokens:

@@ -24,6 +24,7 @@ namespace {
 
 constexpr int kStagingSlots = 4;
 constexpr int kPlanReuseTokens = 32;   // a plan is reused until the batch grew this much per request
+constexpr int64_t kStoreTokens = int64_t(1) << 31;       // more than any pool holds
 constexpr int64_t kDefaultWaitLimitNs = 2000000000ll;   // 2 s: far above any kernel here
 
 struct ProfRecord {
@@ -598,6 +599,153 @@ int32_t odma_ensure_capacity(odma_pool* pool, uint64_t req, int32_t needed_len, 
     pool->last_fused_tensor = false;
     ProfScope ps(pool, ODMA_K_MIGRATE, as_stream(stream));
     return launch_migrate(mp, as_stream(stream)) == cudaSuccess ? ODMA_OK : ODMA_ERR_CUDA;
+}
+
+}  // extern "C"
+
+namespace {
+
+// Bytes of codes and of scales per row; false: no such format for this pool.
+bool store_row(const odma_pool* pool, int32_t format, int32_t group, int64_t* codes, int64_t* scales) {
+    const int64_t D = pool->head_dim;
+    *scales = 0;
+    if (format == ODMA_STORE_RAW) {
+        *codes = D * pool->elem_bytes;
+        return true;
+    }
+    if (format != ODMA_STORE_E4M3 && format != ODMA_STORE_INT8 && format != ODMA_STORE_INT4) return false;
+    if (group < 16 || group > 256 || (group & (group - 1)) != 0 || D % group != 0) return false;
+    *codes = format == ODMA_STORE_INT4 ? D / 2 : D;
+    *scales = D / group * 4;
+    return true;
+}
+
+// A run of tokens of one request.
+struct StoreRun {
+    int64_t base, cap, first, count;
+};
+
+int32_t store_impl(odma_pool* pool, const uint64_t* reqs, const int32_t* first, const int32_t* count, int32_t n, const odma_kv_store* st,
+                   bool pack, void* stream) {
+    if (!pool || !pool->dev_base || !reqs || !st || n < 1) return ODMA_ERR_INVALID;
+    if (st->layer < 0 || st->n_layers < 1 || st->layer > pool->layers - st->n_layers) return ODMA_ERR_INVALID;
+    int64_t row_codes = 0, row_scales = 0;
+    if (!store_row(pool, st->format, st->group, &row_codes, &row_scales)) return ODMA_ERR_INVALID;
+    std::vector<StoreRun> runs;
+    int64_t tokens = 0;
+    try {
+        runs.reserve(n);
+        for (int32_t i = 0; i < n; ++i) {
+            const Request* r = pool->alloc.find(reqs[i]);
+            if (!r) return ODMA_ERR_UNKNOWN_REQ;
+            const int64_t f = first ? first[i] : 0, c = count ? count[i] : r->len - f;
+            if (f < 0 || c < 0) return ODMA_ERR_INVALID;
+            if (f + c > (pack ? r->len : r->cap)) return ODMA_ERR_OVERFLOW;
+            if (c > 0) runs.push_back(StoreRun{r->base, r->cap, f, c});
+            tokens += c;                         // (n below 2^31 runs of at most 2^30 tokens)
+        }
+        if (!pack) {                             // rows that two runs would write
+            std::vector<std::pair<int64_t, int64_t>> to;
+            to.reserve(runs.size());
+            for (const StoreRun& r : runs) to.emplace_back(r.base + r.first, r.base + r.first + r.count);
+            std::sort(to.begin(), to.end());
+            for (size_t i = 1; i < to.size(); ++i)
+                if (to[i].first < to[i - 1].second) return ODMA_ERR_INVALID;
+        }
+    } catch (...) {
+        return ODMA_ERR_NOMEM;
+    }
+    if (tokens == 0) return ODMA_OK;
+    // (a request may be packed any number of times: the products are checked before they are 64-bit numbers)
+    if (tokens >= kStoreTokens || static_cast<__int128>(2) * st->n_layers * tokens * pool->kv_heads * std::max(row_codes, row_scales) >= (int64_t(1) << 62))
+        return ODMA_ERR_INVALID;
+    const int64_t rows = 2ll * st->n_layers * tokens * pool->kv_heads;
+    if (!st->codes || !aligned16(st->codes) || st->codes_bytes < static_cast<uint64_t>(rows * row_codes)) return ODMA_ERR_INVALID;
+    if (row_scales > 0 && (!st->scales || (reinterpret_cast<uintptr_t>(st->scales) & 3u) != 0 || st->scales_bytes < static_cast<uint64_t>(rows * row_scales)))
+        return ODMA_ERR_INVALID;
+    // the store lies apart from the pool, and its halves from one another
+    const int64_t pool_bytes = 2ll * pool->layers * pool->rows_per_array * pool->head_dim * pool->elem_bytes;
+    if (rows_meet(st->codes, rows * row_codes, rows * row_codes, 1, pool->dev_base, pool_bytes)) return ODMA_ERR_INVALID;
+    if (row_scales > 0 && (rows_meet(st->scales, rows * row_scales, rows * row_scales, 1, pool->dev_base, pool_bytes) ||
+                           rows_meet(st->scales, rows * row_scales, rows * row_scales, 1, st->codes, rows * row_codes)))
+        return ODMA_ERR_INVALID;
+    // units of a launch are counted in 31 bits
+    const int64_t per_token = static_cast<int64_t>(pool->kv_heads) *
+                              (st->format == ODMA_STORE_RAW ? pool->head_dim * pool->elem_bytes / 16 : pool->head_dim / 16);
+    const int64_t most = ((int64_t(1) << 31) - (int64_t(1) << 20)) / per_token;
+    if (most < 1) return ODMA_ERR_INVALID;
+    pool->decode_was_last = false;
+    pool->last_fused_tensor = false;
+    ProfScope ps(pool, ODMA_K_MIGRATE, as_stream(stream));
+    for (int32_t l0 = 0; l0 < st->n_layers; l0 += kStoreLayers) {
+        const int32_t layers = std::min(kStoreLayers, st->n_layers - l0);
+        StoreParams p;
+        p.pool = pool->dev_base;
+        p.codes = static_cast<uint8_t*>(st->codes) + 2ll * l0 * tokens * pool->kv_heads * row_codes;
+        p.scales = st->scales ? st->scales + 2ll * l0 * tokens * pool->kv_heads * (row_scales / 4) : nullptr;
+        p.rows_per_array = pool->rows_per_array;
+        p.row0 = 2ll * (st->layer + l0) * pool->rows_per_array;
+        p.store_tokens = tokens;
+        p.arrays = 2 * layers;
+        p.kv_heads = pool->kv_heads;
+        p.head_dim = pool->head_dim;
+        p.group = st->group;
+        for (int32_t l = 0; l < layers; ++l) {
+            const float k = pool->k_scale[st->layer + l0 + l], v = pool->v_scale[st->layer + l0 + l];
+            p.scale[2 * l] = make_float2(k, 1.0f / k);
+            p.scale[2 * l + 1] = make_float2(v, 1.0f / v);
+        }
+        size_t run = 0;
+        int64_t done = 0, token0 = 0;            // of that run; of all
+        while (run < runs.size()) {
+            p.n = 0;
+            p.cu[0] = 0;
+            p.token0 = static_cast<int32_t>(token0);
+            while (run < runs.size() && p.n < kStoreRequests && p.cu[p.n] < most) {
+                const StoreRun& r = runs[run];
+                const int64_t take = std::min(r.count - done, most - p.cu[p.n]);
+                p.row[p.n] = static_cast<int32_t>(r.base * pool->kv_heads + r.first + done);
+                p.cap[p.n] = static_cast<int32_t>(r.cap);
+                p.cu[p.n + 1] = static_cast<int32_t>(p.cu[p.n] + take);
+                ++p.n;
+                done += take;
+                if (done == r.count) {
+                    ++run;
+                    done = 0;
+                }
+            }
+            token0 += p.cu[p.n];
+            if (launch_store(p, st->format, pool->dtype, pack, as_stream(stream)) != cudaSuccess) return ODMA_ERR_CUDA;
+        }
+    }
+    return ODMA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t odma_kv_store_bytes(const odma_pool* pool, int32_t format, int32_t group, int32_t n_layers, int64_t tokens, uint64_t* codes_bytes,
+                            uint64_t* scales_bytes) {
+    int64_t row_codes = 0, row_scales = 0;
+    if (!pool || !codes_bytes || !scales_bytes || n_layers < 1 || n_layers > pool->layers || tokens < 0 || tokens > kStoreTokens ||
+        !store_row(pool, format, group, &row_codes, &row_scales) ||
+        static_cast<__int128>(2) * n_layers * tokens * pool->kv_heads * std::max(row_codes, row_scales) >= (int64_t(1) << 62))
+        return ODMA_ERR_INVALID;
+    const uint64_t rows = 2ull * n_layers * tokens * pool->kv_heads;
+    *codes_bytes = rows * row_codes;
+    *scales_bytes = rows * row_scales;
+    return ODMA_OK;
+}
+
+int32_t odma_pack_kv(odma_pool* pool, const uint64_t* reqs, const int32_t* first, const int32_t* count, int32_t n, const odma_kv_store* store,
+                     void* stream) {
+    return store_impl(pool, reqs, first, count, n, store, true, stream);
+}
+
+int32_t odma_unpack_kv(odma_pool* pool, const uint64_t* reqs, const int32_t* first, const int32_t* count, int32_t n,
+                       const odma_kv_store* store, void* stream) {
+    return store_impl(pool, reqs, first, count, n, store, false, stream);
 }
 
 int32_t odma_free(odma_pool* pool, uint64_t req) {
@@ -1213,6 +1361,137 @@ int32_t odma_decode_attention_prefix(odma_pool* pool, int32_t layer, const void*
     m.v_scale = p.v_scale;
     ProfScope ps(pool, ODMA_K_COMBINE, s);
     return launch_merge_prefix(m, fp32, s) == cudaSuccess ? ODMA_OK : ODMA_ERR_CUDA;
+}
+
+}  // extern "C"
+
+namespace {
+
+// The split and the workspace of a call of odma_prefill_attention.
+struct PrefillShape {
+    bool tensor = false;
+    int32_t tile_tokens = 0, part_rows = 0, shares = 0, min_piece = 0;
+    int64_t wide_tokens = 0;                     // 8-bit pools: tokens widened
+    uint64_t wide_bytes = 0, starts_bytes = 0, part_o_bytes = 0, part_ml_bytes = 0;
+    uint64_t bytes() const { return wide_bytes + starts_bytes + part_o_bytes + part_ml_bytes; }
+};
+
+// Rows of fewer than 33 queries cost little to write and read again, and one step of 128 keys is worth a cut; a full
+// tile's 256 rows are worth six (prefill_plan.cuh).
+int32_t prefill_min_piece(int32_t rows) { return rows <= 32 ? 1 : rows <= 128 ? 2 : 4; }
+
+bool prefill_shape(const odma_pool* pool, int32_t q_heads, const odma_tables* t, PrefillShape* out) {
+    if (!pool || !t || t->n < 1 || t->n > kMaxPrefillBatch || t->n_new_total < 0 || q_heads < pool->kv_heads || q_heads % pool->kv_heads != 0)
+        return false;
+    const int32_t group = q_heads / pool->kv_heads, D = pool->head_dim;
+    if (group > kMaxPrefillGroup || group > pool->alloc.config().max_group || (D != 32 && D != 64 && D != 128)) return false;
+    PrefillShape w;
+    w.tensor = pool->dtype != ODMA_DTYPE_F32 && D != 32;
+    w.tile_tokens = w.tensor ? 2 * (kPrefillRows / 2 / group) : kPrefillPlainRows / group;
+    w.part_rows = std::max(1, std::min(w.tile_tokens, t->n_new_total)) * group;
+    w.shares = w.tensor ? pool->plan_ctas : prefill_plain_blocks() * pool->plan_ctas;
+    w.min_piece = prefill_min_piece(w.part_rows);
+    auto up = [](int64_t b) { return static_cast<uint64_t>((b + 255) / 256 * 256); };
+    if (pool->dtype == ODMA_DTYPE_FP8_E4M3) {
+        // lengths rounded up to 16; on the device's own lengths all the pool can hold
+        w.wide_tokens = built_on_device(t) ? pool->alloc.T() : std::min<int64_t>(pool->alloc.T(), t->kv_tokens + 15ll * t->n);
+        w.wide_bytes = up(2 * w.wide_tokens * pool->kv_heads * D * 2);
+    }
+    w.starts_bytes = up((w.shares + 1ll) * 16);
+    w.part_o_bytes = up(2ll * w.shares * w.part_rows * D * 4);
+    w.part_ml_bytes = up(2ll * w.shares * w.part_rows * 8);
+    *out = w;
+    return true;
+}
+
+// The queries [n_new_total][q_heads][head_dim] by boxes of 64 elements x a KV head's group x a lane's tokens.
+bool make_query_map(const void* q, int64_t tokens, int32_t q_heads, int32_t head_dim, int32_t group, int32_t box_tokens, CUtensorMap* out) {
+    const EncodeTiledFn encode = tensor_map_encoder();
+    if (!encode) return false;
+    const cuuint64_t gdim[3] = {static_cast<cuuint64_t>(head_dim), static_cast<cuuint64_t>(q_heads), static_cast<cuuint64_t>(tokens)};
+    const cuuint64_t gstride[2] = {static_cast<cuuint64_t>(head_dim) * 2, static_cast<cuuint64_t>(head_dim) * 2 * q_heads};
+    const cuuint32_t estride[3] = {1, 1, 1};
+    const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(group), static_cast<cuuint32_t>(box_tokens)};
+    return encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), gdim, gstride, box, estride, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+}  // namespace
+
+extern "C" {
+
+uint64_t odma_prefill_workspace_bytes(const odma_pool* pool, int32_t q_heads, const odma_tables* tables) {
+    PrefillShape w;
+    return prefill_shape(pool, q_heads, tables, &w) ? w.bytes() : 0;
+}
+
+int32_t odma_prefill_attention(odma_pool* pool, int32_t layer, const void* q, int32_t q_heads, const odma_tables* tables,
+                               void* workspace, uint64_t workspace_bytes, void* out, float* lse, void* stream) {
+    int32_t rc = check_decode_args(pool, layer, q, q_heads, tables, out);
+    if (rc != ODMA_OK) return rc;
+    PrefillShape w;
+    if (!prefill_shape(pool, q_heads, tables, &w)) return ODMA_ERR_INVALID;
+    if (tables->n_new_total == 0) return ODMA_OK;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || workspace_bytes < w.bytes()) return ODMA_ERR_INVALID;
+    if ((reinterpret_cast<uintptr_t>(lse) & 3u) != 0) return ODMA_ERR_INVALID;
+    const int32_t D = pool->head_dim;
+    // the queries are read while results are written: they must not meet
+    const int64_t row = static_cast<int64_t>(q_heads) * D * pool->io_bytes, all = row * tables->n_new_total;
+    if (rows_meet(q, all, all, 1, out, all)) return ODMA_ERR_INVALID;
+    DecodeParams d;
+    fill_decode_params(pool, layer, q, q_heads, tables, out, lse, &d);
+    PrefillParams p{};
+    uint8_t* at = static_cast<uint8_t*>(workspace);
+    p.base = d.base;
+    p.cap = d.cap;
+    p.len = d.len;
+    p.cu_new = static_cast<const int32_t*>(tables->d_table) + tables->off_cu_new;
+    p.pool = pool->dev_base;
+    p.q = q;
+    p.out = out;
+    p.lse = lse;
+    p.starts = reinterpret_cast<int4*>(at + w.wide_bytes);
+    p.part_o = reinterpret_cast<float*>(at + w.wide_bytes + w.starts_bytes);
+    p.part_ml = reinterpret_cast<float*>(at + w.wide_bytes + w.starts_bytes + w.part_o_bytes);
+    p.k_row0 = static_cast<int32_t>(2ll * layer * pool->rows_per_array);
+    p.v_row0 = static_cast<int32_t>((2ll * layer + 1) * pool->rows_per_array);
+    p.n = tables->n;
+    p.n_new_total = tables->n_new_total;
+    p.q_heads = q_heads;
+    p.kv_heads = pool->kv_heads;
+    p.group = d.group;
+    p.head_dim = D;
+    p.tile_tokens = w.tile_tokens;
+    p.part_rows = w.part_rows;
+    p.shares = w.shares;
+    p.min_piece = w.min_piece;
+    p.scale_log2 = d.scale_log2 * d.k_scale;
+    p.v_scale = d.v_scale;
+    p.status = pool->d_status;
+    p.wait_limit_ns = kDefaultWaitLimitNs;
+    CUtensorMap q_map, wide_map;
+    if (w.tensor && !make_query_map(q, tables->n_new_total, q_heads, D, d.group, w.tile_tokens / 2, &q_map)) return ODMA_ERR_CUDA;
+    const bool fp8 = w.wide_bytes > 0, fp32 = pool->dtype == ODMA_DTYPE_F32;
+    if (fp8 && !make_tensor_map(workspace, 2 * w.wide_tokens * pool->kv_heads, D, 2, 64, &wide_map)) return ODMA_ERR_CUDA;
+
+    pool->decode_was_last = false;
+    pool->last_fused_tensor = false;
+    cudaStream_t s = as_stream(stream);
+    if (fp8) {
+        p.wide = workspace;
+        p.wide_tokens = w.wide_tokens;
+        ProfScope ps(pool, ODMA_K_DECODE, s);
+        if (launch_prefill_widen(p, s) != cudaSuccess) return ODMA_ERR_CUDA;
+        p.k_row0 = 0;
+        p.v_row0 = static_cast<int32_t>(w.wide_tokens * pool->kv_heads);
+    }
+    {
+        ProfScope ps(pool, ODMA_K_DECODE, s);
+        const cudaError_t e = w.tensor ? launch_prefill_umma(fp8 ? wide_map : pool->maps.box[3], q_map, p, s) : launch_prefill_plain(p, fp32, s);
+        if (e != cudaSuccess) return ODMA_ERR_CUDA;
+    }
+    ProfScope ps(pool, ODMA_K_COMBINE, s);
+    return launch_prefill_merge(p, fp32, s) == cudaSuccess ? ODMA_OK : ODMA_ERR_CUDA;
 }
 
 int32_t odma_decode_attention(odma_pool* pool, int32_t layer, const void* q, int32_t q_heads,

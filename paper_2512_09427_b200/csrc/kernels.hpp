@@ -218,6 +218,66 @@ cudaError_t launch_dequant_prefix(const void* k, const void* v, int64_t head_row
                                   int32_t kv_heads, int32_t head_dim, void* out, cudaStream_t stream);
 cudaError_t launch_merge_prefix(const MergePrefixParams& p, bool fp32, cudaStream_t stream);
 
+// Causal attention of a step's new tokens over the slabs (prefill.cu, prefill_umma.cu).
+struct PrefillParams {
+    const int32_t* base;        // the step's table
+    const int32_t* cap;
+    const int32_t* len;         // tokens after the step
+    const int32_t* cu_new;
+    const void* pool;           // plain-ALU kernel: rows of head_dim elements
+    const void* q;              // [n_new_total, q_heads, head_dim]
+    void* out;
+    float* lse;                 // [n_new_total, q_heads] or nullptr
+    float* part_o;              // [2 shares][part_rows][head_dim] unnormalised
+    float* part_ml;             // [2 shares][part_rows][2] reference (log2 domain) and sum
+    int4* starts;               // [shares + 1] where each share begins: {request, KV head, tile, step}
+    int32_t k_row0, v_row0;     // first row of the layer's K and V array
+    int32_t n, n_new_total, q_heads, kv_heads, group, head_dim;
+    int32_t tile_tokens;        // tokens of a tile of query rows (rows = tokens x group)
+    int32_t part_rows;          // rows of a partial result: of a tile, or all there are
+    int32_t shares;
+    int32_t min_piece;          // steps: a cut closer than this to an end of its tile moves to that end
+    float scale_log2, v_scale;
+    uint32_t* status;
+    int64_t wait_limit_ns;
+    // 8-bit pools: the rows of the requests with new tokens as bf16, [2][wide_tokens x kv_heads], request after
+    // request (lengths rounded up to 16 tokens), head-major inside
+    void* wide;                 // nullptr: the slabs themselves
+    int64_t wide_tokens;        // room; a request that would pass it is refused
+};
+constexpr int kMaxPrefillBatch = 4096;
+constexpr int kMaxPrefillGroup = 64;
+constexpr int kPrefillRows = 256;       // query rows of a tile on the tensor cores, in two lanes of half as many
+constexpr int kPrefillStep = 128;       // keys per step
+constexpr int kPrefillPlainRows = 64;   // and of the plain-ALU kernel
+constexpr int kPrefillPlainStep = 64;
+int32_t prefill_plain_blocks();         // blocks of the plain-ALU kernel that an SM holds
+cudaError_t launch_prefill_umma(const CUtensorMap& kv, const CUtensorMap& q, const PrefillParams& p, cudaStream_t stream);
+cudaError_t launch_prefill_plain(const PrefillParams& p, bool fp32, cudaStream_t stream);
+cudaError_t launch_prefill_widen(const PrefillParams& p, cudaStream_t stream);
+cudaError_t launch_prefill_merge(const PrefillParams& p, bool fp32, cudaStream_t stream);
+
+// Rows of slabs to and from a dense store in fewer bits (store.cu).
+constexpr int kStoreRequests = 128;     // of one launch; more go in several
+constexpr int kStoreLayers = 32;
+struct StoreParams {
+    void* pool;
+    void* codes;                // of the launch's first layer
+    float* scales;
+    int64_t rows_per_array;
+    int64_t row0;               // first row of the launch's first array
+    int64_t store_tokens;       // tokens of the whole store: its arrays lie that many rows apart
+    int32_t arrays;             // layers * 2
+    int32_t n, kv_heads, head_dim, group;   // group: elements per scale
+    int32_t token0;             // store token of the launch's first
+    int32_t cu[kStoreRequests + 1];         // the launch's tokens of the requests ahead
+    int32_t row[kStoreRequests];            // row of KV head 0 and the request's first token inside one array
+    int32_t cap[kStoreRequests];
+    float2 scale[2 * kStoreLayers];         // 8-bit pools: {scale, 1 / scale} of every array
+};
+// `format` as in odma.h; `dtype` of the pool; `pack`: out of the slabs.
+cudaError_t launch_store(const StoreParams& p, int format, int dtype, bool pack, cudaStream_t stream);
+
 struct MigrateParams {
     void* pool;
     int64_t rows_per_array;

@@ -1,0 +1,249 @@
+// The split of a step's causal attention over the blocks of one launch, worked out by every block for
+// itself from the lengths in the step's table.  Included by .cu files only.
+//
+// Work is a list of tiles: request by request, KV head by KV head, `tile_tokens` new tokens at a time.
+// Tile j of a request with c tokens before the step sees the keys up to its last token, in steps of
+// STEP keys.  In units of 1 / STEP of a step it is charged c + tile_tokens * (j + 1) + STEP * kStart, so that
+// the tiles before the j-th cost
+//     F(j) = j (c + STEP * kStart) + tile_tokens j (j + 1) / 2
+// and share s of S, which begins at cost s * ceil(total / S), is found by three searches in closed form.  A
+// share that begins inside a tile cuts it: the pieces leave partial results and a second kernel merges them.
+// A cut costs about kCut steps (its rows are written in 32 bits and read again), so when there are no more
+// tiles than shares and the longest tile ends before an equal share and a cut would, every share takes a
+// tile; and a cut closer than `min_piece` steps to an end of its tile moves to that end.
+#pragma once
+
+#include "device_utils.cuh"
+
+namespace odma {
+namespace dev {
+
+constexpr int kPlanStart = 3;       // steps: what beginning and ending a tile costs
+constexpr int kPlanCut = 6;         // steps: what a cut costs, rows in 32 bits and their merge
+
+struct alignas(16) PlanScratch {                // shared memory of one block
+    int64_t sums[3][32];
+    int64_t total_cost, total_tiles;
+    int32_t longest, wide_at;
+    int4 cut[2];
+};
+
+__device__ __forceinline__ int prefill_tiles(int new_tokens, int tile_tokens) { return (new_tokens + tile_tokens - 1) / tile_tokens; }
+
+// New tokens of request i, 0 where its words do not fit together (a refused request has length 0).
+__device__ __forceinline__ int prefill_new(const PrefillParams& p, int i, int len) {
+    const int add = __ldg(p.cu_new + i + 1) - __ldg(p.cu_new + i);
+    return add > 0 && add <= len ? add : 0;
+}
+
+// Where this block's share begins and ends: cut[0], cut[1] = {request, head, tile, step}; a request of n: behind
+// everything; wide_at: see PrefillItem, of the first.  `cum` and `lens` [n] and, for an 8-bit pool, `wide_of` [n] are scratch.
+// Every thread of the block calls; a barrier is behind the last access.
+template <int STEP, int THREADS>
+__device__ void prefill_plan(const PrefillParams& p, PlanScratch* s, int64_t* cum, int32_t* lens, int32_t* wide_of) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int per = (p.n + THREADS - 1) / THREADS;
+    constexpr int64_t OV = static_cast<int64_t>(STEP) * kPlanStart;
+    // a thread takes `per` requests in a row
+    auto tile_sum = [&](int64_t ctx, int64_t j) { return j * (ctx + OV) + static_cast<int64_t>(p.tile_tokens) * (j * (j + 1) / 2); };
+    int64_t cost = 0, tiles = 0, wide = 0;
+    int longest = 0;
+    for (int k = 0; k < per; ++k) {
+        const int i = tid * per + k;
+        if (i >= p.n) break;
+        const int len = __ldg(p.len + i), add = prefill_new(p, i, len), nt = prefill_tiles(add, p.tile_tokens);
+        cost += tile_sum(len - add, nt) * p.kv_heads;
+        tiles += static_cast<int64_t>(nt) * p.kv_heads;
+        if (add > 0) {
+            wide += (len + 15) & ~15;
+            longest = max(longest, (len + STEP - 1) / STEP);
+        }
+    }
+    auto warp_scan = [&](int64_t v) {
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t x = __shfl_up_sync(0xFFFFFFFFu, v, o);
+            if (lane >= o) v += x;
+        }
+        return v;
+    };
+    int64_t cost_to = warp_scan(cost), tiles_to = warp_scan(tiles), wide_to = warp_scan(wide);
+    longest = __reduce_max_sync(0xFFFFFFFFu, longest);
+    if (tid == 0) s->longest = 0;
+    if (lane == 31) {
+        s->sums[0][warp] = cost_to;
+        s->sums[1][warp] = tiles_to;
+        s->sums[2][warp] = wide_to;
+    }
+    __syncthreads();
+    if (lane == 0) atomicMax(&s->longest, longest);
+    if (warp == 0) {
+        const bool in = lane < THREADS / 32;
+        const int64_t a = warp_scan(in ? s->sums[0][lane] : 0), b = warp_scan(in ? s->sums[1][lane] : 0),
+                      c = warp_scan(in ? s->sums[2][lane] : 0);
+        if (in) {
+            s->sums[0][lane] = a;
+            s->sums[1][lane] = b;
+            s->sums[2][lane] = c;
+        }
+        if (lane == 31) {
+            s->total_cost = a;
+            s->total_tiles = b;
+        }
+    }
+    __syncthreads();
+    if (warp > 0) {
+        cost_to += s->sums[0][warp - 1];
+        tiles_to += s->sums[1][warp - 1];
+        wide_to += s->sums[2][warp - 1];
+    }
+    const int64_t total_cost = s->total_cost, total_tiles = s->total_tiles, S = p.shares;
+    // a tile each, or shares of equal cost
+    const bool whole = total_tiles <= S && static_cast<int64_t>(s->longest + kPlanStart) * STEP * S <= total_cost + kPlanCut * STEP * S;
+    int64_t at = (whole ? tiles_to - tiles : cost_to - cost), wide_at = wide_to - wide;
+    for (int k = 0; k < per; ++k) {
+        const int i = tid * per + k;
+        if (i >= p.n) break;
+        const int len = __ldg(p.len + i), add = prefill_new(p, i, len), nt = prefill_tiles(add, p.tile_tokens);
+        cum[i] = at;
+        lens[i] = len;
+        if (p.wide) {
+            wide_of[i] = static_cast<int32_t>(min(wide_at, p.wide_tokens));
+            if (add > 0) wide_at += (len + 15) & ~15;
+        }
+        at += whole ? static_cast<int64_t>(nt) * p.kv_heads : tile_sum(len - add, nt) * p.kv_heads;
+    }
+    __syncthreads();
+    if (tid < 2) {
+        const int64_t total = whole ? total_tiles : total_cost;
+        int64_t share = 1;
+        if (!whole) {
+            share = (total + S - 1) / S;
+            const int64_t least = static_cast<int64_t>(p.min_piece + kPlanStart) * STEP;
+            if (share < least) share = least;
+        }
+        const int64_t x = (static_cast<int64_t>(blockIdx.x) + tid) * share;
+        int4 c = make_int4(p.n, 0, 0, 0);
+        if (x < total && !(static_cast<int>(blockIdx.x) + tid == p.shares)) {
+            int lo = 0, hi = p.n;                       // the last request whose cost before it is at most x
+            while (hi - lo > 1) {
+                const int mid = (lo + hi) >> 1;
+                if (cum[mid] <= x) lo = mid; else hi = mid;
+            }
+            c.x = lo;
+            const int len = lens[lo], add = prefill_new(p, lo, len), ctx = len - add, nt = prefill_tiles(add, p.tile_tokens);
+            const int64_t head_cost = whole ? nt : tile_sum(ctx, nt);
+            int64_t y = x - cum[lo];
+            c.y = static_cast<int>(y / head_cost);
+            y -= c.y * head_cost;
+            if (whole) {
+                c.z = static_cast<int>(y);
+            } else {
+                int a = 0, b = nt;                      // the last tile with F(tile) <= y
+                while (b - a > 1) {
+                    const int mid = (a + b) >> 1;
+                    if (tile_sum(ctx, mid) <= y) a = mid; else b = mid;
+                }
+                c.z = a;
+                const int64_t before = tile_sum(ctx, a), tile_cost = tile_sum(ctx, a + 1) - before;
+                const int steps = (ctx + min((a + 1) * p.tile_tokens, add) + STEP - 1) / STEP;
+                int t = static_cast<int>((y - before) * steps / tile_cost);
+                bool next = false;
+                if (steps < 2 * p.min_piece) {
+                    next = 2 * t >= steps;
+                    t = 0;
+                } else if (t < p.min_piece) {
+                    t = 0;
+                } else if (t > steps - p.min_piece) {
+                    next = true;
+                }
+                c.w = next ? 0 : t;
+                if (next && ++c.z == nt) {
+                    c.z = 0;
+                    if (++c.y == p.kv_heads) {
+                        c.y = 0;
+                        for (++c.x; c.x < p.n && prefill_new(p, c.x, lens[c.x]) == 0;) ++c.x;
+                    }
+                }
+            }
+        }
+        s->cut[tid] = c;
+        if (tid == 0) s->wide_at = p.wide && c.x < p.n ? wide_of[c.x] : 0;
+        if (tid == 0) p.starts[blockIdx.x] = c;
+        if (tid == 1 && static_cast<int>(blockIdx.x) + 1 == p.shares) p.starts[p.shares] = c;
+    }
+    __syncthreads();
+}
+
+// One piece of work: steps [t0, t1) of a tile.
+struct PrefillItem {
+    int request, head;
+    int tok0;               // first token of the tile among the request's new ones
+    int add, ctx;           // new tokens and tokens before them
+    int cu;                 // the request's first row of q
+    int t0, t1;             // t1 = 0: no more items
+    int slot;               // partial result, -1: the tile is whole
+    int base, cap;
+    int wide_at;            // 8-bit pools: the request's first token in the widened rows
+};
+
+// Walks the items of a share.  Called by one whole warp (or by every thread, which then reads the same words).
+template <int STEP>
+struct PrefillWalk {
+    const PrefillParams& p;
+    int4 at, end;
+    int len, add, ctx, cu, base, cap, wide_at;
+
+    __device__ __forceinline__ PrefillWalk(const PrefillParams& params, const PlanScratch& s)
+        : p(params), at(s.cut[0]), end(s.cut[1]), wide_at(s.wide_at) {
+        if (at.x < p.n) fetch();
+    }
+    __device__ __forceinline__ void fetch() {
+        len = __ldg(p.len + at.x);
+        add = prefill_new(p, at.x, len);
+        ctx = len - add;
+        cu = __ldg(p.cu_new + at.x);
+        base = __ldg(p.base + at.x);
+        cap = __ldg(p.cap + at.x);
+    }
+    __device__ __forceinline__ bool next(PrefillItem& it) {
+        if (at.x >= p.n || (at.x == end.x && at.y == end.y && at.z == end.z && at.w == end.w)) return false;
+        const bool last = at.x == end.x && at.y == end.y && at.z == end.z;      // the share ends inside this tile
+        const int tok0 = at.z * p.tile_tokens;
+        const int steps = (ctx + min(tok0 + p.tile_tokens, add) + STEP - 1) / STEP;
+        it.request = at.x;
+        it.head = at.y;
+        it.tok0 = tok0;
+        it.add = add;
+        it.ctx = ctx;
+        it.cu = cu;
+        it.t0 = at.w;
+        it.t1 = last ? end.w : steps;
+        it.slot = at.w > 0 ? 2 * static_cast<int>(blockIdx.x) : last ? 2 * static_cast<int>(blockIdx.x) + 1 : -1;
+        it.base = base;
+        it.cap = cap;
+        it.wide_at = wide_at;
+        if (last) {
+            at = end;
+        } else {
+            at.w = 0;
+            if ((at.z + 1) * p.tile_tokens < add) {
+                ++at.z;
+            } else {
+                at.z = 0;
+                if (++at.y == p.kv_heads) {
+                    at.y = 0;
+                    wide_at += (len + 15) & ~15;
+                    for (++at.x; at.x < p.n; ++at.x) {
+                        fetch();
+                        if (add > 0) break;
+                    }
+                }
+            }
+        }
+        return true;
+    }
+};
+
+}  // namespace dev
+}  // namespace odma

@@ -24,6 +24,7 @@ OK, ERR_INVALID, ERR_NOMEM, ERR_UNKNOWN_REQ, ERR_DUP_REQ, ERR_OVERFLOW, ERR_CUDA
 DTYPE_F32, DTYPE_BF16, DTYPE_FP8_E4M3 = 0, 1, 2
 DECODE_AUTO, DECODE_TCGEN05, DECODE_MMA_SYNC = 0, 1, 2
 READOUT_AUTO, READOUT_LATE, READOUT_AT_ONCE = 0, 1, 2
+STORE_RAW, STORE_E4M3, STORE_INT8, STORE_INT4 = 0, 1, 2, 3
 K_APPEND, K_DECODE, K_COMBINE, K_MIGRATE, K_PROBE = range(5)
 
 
@@ -97,6 +98,16 @@ class QkvPrep(C.Structure):
                          v_stride, pos_stride, rot_dim, int(interleaved), max(1, len(section)), (C.c_int32 * 4)(*section), eps)
 
 
+class KvStore(C.Structure):
+    """odma_kv_store: where odma_pack_kv leaves rows and odma_unpack_kv finds them.  Pointers as integers, sizes in bytes."""
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p), ("codes_bytes", C.c_uint64), ("scales_bytes", C.c_uint64),
+                ("format", C.c_int32), ("group", C.c_int32), ("layer", C.c_int32), ("n_layers", C.c_int32)]
+
+    def __init__(self, format: int, group: int, layer: int, n_layers: int, codes: int, codes_bytes: int, scales: int = 0,
+                 scales_bytes: int = 0):
+        super().__init__(codes or None, scales or None, codes_bytes, scales_bytes, format, group, layer, n_layers)
+
+
 SIM_STATIC, SIM_PAGED16, SIM_ODMA = 0, 1, 2
 
 _vp, _i32, _u64, _i64 = C.c_void_p, C.c_int32, C.c_uint64, C.c_int64
@@ -124,6 +135,11 @@ _SIGS = {
     "odma_plan_host": (_i32, [_vp, _u64p, _i32p, _i32, _i32p, _u64, C.POINTER(Tables)]),
     "odma_build_tables": (_i32, [_vp, _u64p, _i32p, _i32, _vp, _u64, _vp, C.POINTER(Tables)]),
     "odma_build_prefill_tables": (_i32, [_vp, _u64p, _i32p, _i32, _vp, _u64, _vp, C.POINTER(Tables)]),
+    "odma_prefill_workspace_bytes": (_u64, [_vp, _i32, C.POINTER(Tables)]),
+    "odma_prefill_attention": (_i32, [_vp, _i32, _vp, _i32, C.POINTER(Tables), _vp, _u64, _vp, _vp, _vp]),
+    "odma_kv_store_bytes": (_i32, [_vp, _i32, _i32, _i32, _i64, _u64p, _u64p]),
+    "odma_pack_kv": (_i32, [_vp, _u64p, _i32p, _i32p, _i32, C.POINTER(KvStore), _vp]),
+    "odma_unpack_kv": (_i32, [_vp, _u64p, _i32p, _i32p, _i32, C.POINTER(KvStore), _vp]),
     "odma_slab_table": (_i32, [_vp, _u64p, _i32, _vp, _vp, _vp]),
     "odma_build_tables_device": (_i32, [_vp, _vp, _vp, _vp, _i32, _i32, _vp, _u64, _vp, _vp, _vp, _vp, C.POINTER(Tables)]),
     "odma_append_qkv": (_i32, [_vp, _i32, C.POINTER(Tables), _vp, _vp, _vp, _vp, _i32, C.POINTER(QkvPrep), _vp]),
@@ -295,6 +311,25 @@ class Pool:
                                               table_bytes, stream or None, C.byref(t)), "odma_build_prefill_tables")
         return t
 
+    def kv_store_bytes(self, format: int, group: int, n_layers: int, tokens: int) -> Tuple[int, int]:
+        """Bytes of codes and of scales that `tokens` tokens of n_layers layers take in a store."""
+        codes, scales = C.c_uint64(), C.c_uint64()
+        _check(_lib.odma_kv_store_bytes(self._h, format, group, n_layers, tokens, C.byref(codes), C.byref(scales)),
+               "odma_kv_store_bytes")
+        return int(codes.value), int(scales.value)
+
+    def pack_kv(self, reqs: Sequence[int], store: KvStore, first: Optional[Sequence[int]] = None,
+                count: Optional[Sequence[int]] = None, stream: int = 0) -> None:
+        """Rows of the requests' slabs to a dense store (first: 0 each; count: up to the committed length)."""
+        _check(_lib.odma_pack_kv(self._h, _u64arr(reqs), _i32arr(first), _i32arr(count), len(reqs), C.byref(store),
+                                 stream or None), "odma_pack_kv")
+
+    def unpack_kv(self, reqs: Sequence[int], store: KvStore, first: Optional[Sequence[int]] = None,
+                  count: Optional[Sequence[int]] = None, stream: int = 0) -> None:
+        """Rows from a store back into slabs; lengths are not committed."""
+        _check(_lib.odma_unpack_kv(self._h, _u64arr(reqs), _i32arr(first), _i32arr(count), len(reqs), C.byref(store),
+                                   stream or None), "odma_unpack_kv")
+
     def slab_table(self, reqs: Sequence[int], d_slabs: int, d_len: int = 0, stream: int = 0) -> None:
         """Slabs ([n][2]: base, capacity) and committed lengths of live requests to device memory."""
         _check(_lib.odma_slab_table(self._h, _u64arr(reqs), len(reqs), d_slabs, d_len or None, stream or None),
@@ -316,6 +351,15 @@ class Pool:
         """Norm and rotation of the step's query and key heads, queries to q_out, keys and values to the slabs."""
         _check(_lib.odma_append_qkv(self._h, layer, C.byref(tables), q, k_new, v_new, q_out, q_heads, C.byref(prep),
                                     stream or None), "odma_append_qkv")
+
+    def prefill_workspace_bytes(self, q_heads: int, tables: Tables) -> int:
+        return int(_lib.odma_prefill_workspace_bytes(self._h, q_heads, C.byref(tables)))
+
+    def prefill_attention(self, layer: int, q: int, q_heads: int, tables: Tables, workspace: int, workspace_bytes: int, out: int,
+                          lse: int = 0, stream: int = 0) -> None:
+        """Causal attention of the step's new tokens (appended through the same tables) over the requests' slabs."""
+        _check(_lib.odma_prefill_attention(self._h, layer, q, q_heads, C.byref(tables), workspace or None, workspace_bytes,
+                                           out, lse or None, stream or None), "odma_prefill_attention")
 
     def prefix_workspace_bytes(self, q_heads: int, n: int, prefix_len: int) -> int:
         return int(_lib.odma_prefix_workspace_bytes(self._h, q_heads, n, prefix_len))
