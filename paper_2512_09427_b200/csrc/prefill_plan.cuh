@@ -3,12 +3,12 @@
 //
 // Work is a list of tiles: request by request, KV head by KV head, `tile_tokens` new tokens at a time.
 // Tile j of a request with c tokens before the step sees the keys up to its last token, in steps of
-// STEP keys.  In units of 1 / STEP of a step it is charged c + tile_tokens * (j + 1) + STEP * kStart, so that
+// STEP keys.  In units of 1 / STEP of a step it is charged c + tile_tokens * (j + 1) + start, so that
 // the tiles before the j-th cost
-//     F(j) = j (c + STEP * kStart) + tile_tokens j (j + 1) / 2
+//     F(j) = j (c + start) + tile_tokens j (j + 1) / 2
 // and share s of S, which begins at cost s * ceil(total / S), is found by three searches in closed form.  A
 // share that begins inside a tile cuts it: the pieces leave partial results and a second kernel merges them.
-// A cut costs about kCut steps (its rows are written in 32 bits and read again), so when there are no more
+// A cut costs about six steps (its rows are written in 32 bits and read again), so when there are no more
 // tiles than shares and the longest tile ends before an equal share and a cut would, every share takes a
 // tile; and a cut closer than `min_piece` steps to an end of its tile moves to that end.
 #pragma once
@@ -18,8 +18,8 @@
 namespace odma {
 namespace dev {
 
-constexpr int kPlanStart = 3;       // steps: what beginning and ending a tile costs
-constexpr int kPlanCut = 6;         // steps: what a cut costs, rows in 32 bits and their merge
+constexpr int kPlanStart = 13;      // eighths of a step: what beginning and ending a tile costs, and half a step for its last one
+constexpr int kPlanCut = 48;        // what a cut costs: rows in 32 bits and their merge
 
 struct alignas(16) PlanScratch {                // shared memory of one block
     int64_t sums[3][32];
@@ -43,7 +43,7 @@ template <int STEP, int THREADS>
 __device__ void prefill_plan(const PrefillParams& p, PlanScratch* s, int64_t* cum, int32_t* lens, int32_t* wide_of) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = (p.n + THREADS - 1) / THREADS;
-    constexpr int64_t OV = static_cast<int64_t>(STEP) * kPlanStart;
+    constexpr int64_t OV = STEP / 8 * kPlanStart, CUT = STEP / 8 * kPlanCut;
     // a thread takes `per` requests in a row
     auto tile_sum = [&](int64_t ctx, int64_t j) { return j * (ctx + OV) + static_cast<int64_t>(p.tile_tokens) * (j * (j + 1) / 2); };
     int64_t cost = 0, tiles = 0, wide = 0;
@@ -99,7 +99,7 @@ __device__ void prefill_plan(const PrefillParams& p, PlanScratch* s, int64_t* cu
     }
     const int64_t total_cost = s->total_cost, total_tiles = s->total_tiles, S = p.shares;
     // a tile each, or shares of equal cost
-    const bool whole = total_tiles <= S && static_cast<int64_t>(s->longest + kPlanStart) * STEP * S <= total_cost + kPlanCut * STEP * S;
+    const bool whole = total_tiles <= S && (static_cast<int64_t>(s->longest) * STEP + OV) * S <= total_cost + CUT * S;
     int64_t at = (whole ? tiles_to - tiles : cost_to - cost), wide_at = wide_to - wide;
     for (int k = 0; k < per; ++k) {
         const int i = tid * per + k;
@@ -119,7 +119,7 @@ __device__ void prefill_plan(const PrefillParams& p, PlanScratch* s, int64_t* cu
         int64_t share = 1;
         if (!whole) {
             share = (total + S - 1) / S;
-            const int64_t least = static_cast<int64_t>(p.min_piece + kPlanStart) * STEP;
+            const int64_t least = static_cast<int64_t>(p.min_piece) * STEP + OV;
             if (share < least) share = least;
         }
         const int64_t x = (static_cast<int64_t>(blockIdx.x) + tid) * share;

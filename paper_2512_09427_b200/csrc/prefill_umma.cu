@@ -10,19 +10,18 @@
 // and both lanes use every step's K and V.  The lanes are out of phase: while one's softmax runs, the tensor pipe
 // has the other's products.
 //
-// Tensor memory (512 columns): a lane has S (128 columns) and O (D columns); P (bf16) overwrites S from the left, 16
-// columns for the 32 just read.
+// Tensor memory (512 columns): a lane has S (128 columns) and O (D columns); P (bf16) overwrites S from the left, 32
+// columns for the 64 just read.
 //
-// Warps 0-3 and 4-7: softmax of lane 0 and 1, a thread per row; warp 8: TMA producer; warps 9 and 10: issue of lane 0's
-// and 1's products, QK(0), then PV(u) QK(u + 1) for every step u, so S is only overwritten by a product issued after the one
-// that reads P from it.
+// Warps 0-3 and 4-7: softmax of lane 0 and 1, a thread per row; warp 8: TMA producer; warp 9: issue of the products, QK(0) of
+// both lanes, then PV(u) QK(u + 1) of one and of the other for every step u, so S is only overwritten by a product issued
+// after the one that reads P from it; warp 10 does the issuing warp's waits for loads and hands stages back.
 //
 // The softmax keeps a reference m per row, raised only when a maximum passes it by 2^8: P stays below 256, which bf16
-// relative to the fp32 accumulator does not mind.  So the 32 columns of a chunk need not wait for the other 96: the weights
-// are computed with the standing reference while the chunk's maximum is found, and where it turns out too low (a tile's
-// first chunk, and rarely later) the chunk is done again and what is already there, sum, O, and P of the step, is scaled.
-// P is rounded to bf16 for the product (half a step: at most 2^-8 of a weight, random in sign over the keys); sums,
-// maxima and O are fp32.
+// relative to the fp32 accumulator does not mind.  So the weights need not wait for the maximum: both are found at once, with
+// the standing reference, for one half of a step and then the other, and where the reference turns out too low (in a tile's
+// first half step, and rarely later) the half is done again and sum and O are scaled.  P is rounded to bf16 for the product
+// (half a step: at most 2^-8 of a weight, random in sign over the keys); sums, maxima and O are fp32.
 #include "odma.h"
 #include "prefill_plan.cuh"
 #include "tcgen05.cuh"
@@ -35,16 +34,17 @@ using namespace dev;
 constexpr int kM = kPrefillRows / 2;                // rows per lane
 constexpr int kStep = kPrefillStep;
 constexpr int kChunk = 32;                          // scores of a row in registers at a time
-constexpr int kThreads = 384;
-constexpr int kProducerWarp = 8, kMmaWarp = 9;      // and kMmaWarp + 1
+constexpr int kSoftmaxWarps = 8;                    // lane 0 and 1, four times 32 rows
+constexpr int kProducerWarp = kSoftmaxWarps, kMmaWarp = kSoftmaxWarps + 1;
+constexpr int kThreads = (kSoftmaxWarps + 2) * 32;
 constexpr int kMaxStages = 10;
 constexpr int kItemSlots = 4;
-constexpr float kRescaleAbove = 8.f;
+constexpr float kRaiseAbove = 16.f, kTooLarge = 65536.f;         // how far a maximum, in log2, or a half step's sum of weights may pass the reference
 constexpr int kHalfBytes = 128 * 128;               // 64 elements of 128 rows: of a lane's queries, of a step's keys or values
 // barriers
 constexpr int kBarFull = 0, kBarEmpty = kMaxStages, kBarItem = 2 * kMaxStages, kBarQFull = kBarItem + kItemSlots,
-              kBarQFree = kBarQFull + 1, kBarS = kBarQFree + 1, kBarPa = kBarS + 2, kBarPb = kBarPa + 2, kBarHalf = kBarPb + 2,
-              kBarO = kBarHalf + 2, kBarDrain = kBarO + 2, kNumBars = kBarDrain + 2;
+              kBarQFree = kBarQFull + 2, kBarS = kBarQFree + 2, kBarPa = kBarS + 2, kBarPb = kBarPa + 2, kBarHalf = kBarPb + 2,
+              kBarO = kBarHalf + 2, kBarDrain = kBarO + 2, kNumBars = kBarDrain + 1;
 
 template <int D>
 struct Config {
@@ -66,62 +66,30 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
         : "memory");
 }
 
-// Maxima that a NaN goes through.
-__device__ __forceinline__ float max3(float a, float b, float c) {
-    float d;
-    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
-    return d;
-}
 __device__ __forceinline__ float row_max(const uint32_t (&s)[kChunk]) {
     float mx[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) mx[k] = __uint_as_float(s[k]);
 #pragma unroll
-    for (int i = 4; i < kChunk - 4; i += 8)
+    for (int i = 4; i < kChunk; i += 4)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) mx[k] = max3(mx[k], __uint_as_float(s[i + 2 * k]), __uint_as_float(s[i + 2 * k + 1]));
-    const float a = max3(mx[0], __uint_as_float(s[kChunk - 4]), __uint_as_float(s[kChunk - 3])),
-                b = max3(mx[1], __uint_as_float(s[kChunk - 2]), __uint_as_float(s[kChunk - 1]));
-    return max3(a, b, max3(mx[2], mx[3], mx[3]));
+        for (int k = 0; k < 4; ++k) mx[k] = fmaxf(mx[k], __uint_as_float(s[i + k]));
+    return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
 }
 
-// 2^x on the fused multiply-add pipe, for finite x <= 127: x = n + f with |f| <= 1/2, 2^f by the polynomial of degree 4
-// with the least relative error on that interval (2.6e-6, far below the rounding of P), n added to the exponent.  Below 2^-126 the
-// result is some number below 2^-125.  Two at a time.
-__device__ __forceinline__ float2 poly_exp2(float2 x) {
-    x.x = fmaxf(x.x, -126.f);
-    x.y = fmaxf(x.y, -126.f);
-    const float2 round = make_float2(12582912.f, 12582912.f), back = make_float2(-12582912.f, -12582912.f);
-    const float2 t = add2(x, round), n = add2(t, back);
-    const float2 f = fma2(n, make_float2(-1.f, -1.f), x);
-    float2 y = fma2(f, make_float2(0.0095701f, 0.0095701f), make_float2(0.05591786f, 0.05591786f));
-    y = fma2(y, f, make_float2(0.24024745f, 0.24024745f));
-    y = fma2(y, f, make_float2(0.69312181f, 0.69312181f));
-    y = fma2(y, f, make_float2(0.99999926f, 0.99999926f));
-    return make_float2(__uint_as_float(__float_as_uint(y.x) + (__float_as_uint(t.x) << 23)),
-                       __uint_as_float(__float_as_uint(y.y) + (__float_as_uint(t.y) << 23)));
-}
-
-// Weights 2^(s * scale - ref) of a chunk, rounded to bf16, and their sum (unrounded).  The first POLY of its 16 pairs
-// take the fused multiply-add pipe, the others the special-function unit.
-template <int POLY>
+// Weights 2^(s * scale - ref) of a chunk, rounded to bf16, and their sum (unrounded).
 __device__ __forceinline__ float weights(const uint32_t (&s)[kChunk], float scale, float ref, uint32_t (&pk)[kChunk / 2]) {
     const float2 sc = make_float2(scale, scale), neg = make_float2(-ref, -ref);
     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
     for (int i = 0; i < kChunk / 2; ++i) {
         float2 x = fma2(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), sc, neg);
-        if (i * POLY / 16 != (i + 1) * POLY / 16)
-            x = poly_exp2(x);
-        else
-            x = make_float2(fast_exp2(x.x), fast_exp2(x.y));
+        x = make_float2(fast_exp2(x.x), fast_exp2(x.y));
         sum[i & 1] = add2(sum[i & 1], x);
         pk[i] = pack_bf16(x.x, x.y);
     }
     return (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
 }
-constexpr int kPolyPairs = 5;
-
 // 32 bytes, a whole sector, in one instruction.
 __device__ __forceinline__ void store8(void* p, const uint32_t* v) {
     asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
@@ -155,9 +123,8 @@ prefill_umma_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_con
     // ---- set-up: barriers, tensor memory, query rows that no token has, the share
     if (warp == kProducerWarp) {
         for (int i = lane; i < kNumBars; i += 32) {
-            const bool softmax = i >= kBarPa && i < kBarHalf;                    // a lane's four softmax warps
-            const bool both = (i >= kBarEmpty && i < kBarItem) || i == kBarQFree;
-            mbar_init(bar(i), softmax ? 4u : both ? 2u : 1u);
+            const bool free = i == kBarQFree || i == kBarQFree + 1;          // a lane's softmax warps; and its last product
+            mbar_init(bar(i), free ? 5u : i >= kBarPa && i < kBarHalf ? 4u : 1u);
         }
         if (lane == 0) *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -165,7 +132,7 @@ prefill_umma_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_con
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512u)
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    } else if (warp < 8) {
+    } else if (warp < kSoftmaxWarps) {
         const int spare = (kM - lane_rows) * 8 * Cfg::kHalves;                   // 16-byte chunks behind a lane's rows
         uint8_t* q_lane = qbuf + (warp >> 2) * Cfg::kQBytes;
         for (int i = tid & 127; i < spare; i += 128) {
@@ -216,7 +183,8 @@ prefill_umma_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_con
         };
         bool more = walk.next(it);
         while (ok) {
-            // The slot's last item lies four back: its readers have all come to a later one (see the waits on kBarQFree).
+            // The slot's last item lies four back, and both lanes' softmax warps have read the one two back (they arrive on
+            // kBarQFree when they have; the issuing warp is ahead of them).
             PrefillItem* to = items + (n_items & (kItemSlots - 1));
             if (!more) it.t1 = 0;
             if (lane == 0) {
@@ -229,24 +197,27 @@ prefill_umma_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_con
                                  static_cast<int64_t>(it.head) * (p.wide ? (it.ctx + it.add + 15) & ~15 : it.cap);
             k_row = static_cast<int32_t>(p.k_row0 + rows);
             v_row = static_cast<int32_t>(p.v_row0 + rows);
-            load(false, it.t0);
-            // the queries, once the products of the item before have read theirs
-            if (ok && n_items > 0)
-                ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(kBarQFree), static_cast<uint32_t>(n_items - 1) & 1u, abort_flag, p.status, limit));
-            if (!ok) break;
-            const int lanes = it.tok0 + lane_tokens < it.add ? 2 : 1;
-            if (lane == 0) mbar_expect_tx(bar(kBarQFull), static_cast<uint32_t>(lanes * Cfg::kHalves * lane_rows * 128));
-            __syncwarp();
-            if (lane < lanes * Cfg::kHalves) {
-                const int L = lane / Cfg::kHalves, hf = lane % Cfg::kHalves;
-                tma_load_3d(q_u32 + L * Cfg::kQBytes + hf * kHalfBytes, &q_map, hf * 64, it.head * p.group, it.cu + it.tok0 + L * lane_tokens,
-                            bar(kBarQFull));
-            }
-            ++n_items;
+            // a lane's queries, once its products of the item before have read theirs
+            auto queries = [&](int L) {
+                if (ok && n_items > 0)
+                    ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(kBarQFree + L), static_cast<uint32_t>(n_items - 1) & 1u, abort_flag, p.status, limit));
+                if (!ok) return;
+                const bool some = it.tok0 + L * lane_tokens < it.add;
+                if (lane == 0) mbar_expect_tx(bar(kBarQFull + L), some ? static_cast<uint32_t>(Cfg::kHalves * lane_rows * 128) : 0u);
+                __syncwarp();
+                if (some && lane < Cfg::kHalves)
+                    tma_load_3d(q_u32 + L * Cfg::kQBytes + lane * kHalfBytes, &q_map, lane * 64, it.head * p.group, it.cu + it.tok0 + L * lane_tokens,
+                                bar(kBarQFull + L));
+            };
             const int t0 = it.t0, t1 = it.t1;
-            for (int u = t0; u < t1 && ok; ++u) {
-                load(true, u);
-                if (ok && u + 1 < t1) load(false, u + 1);
+            load(false, t0);
+            queries(0);
+            if (ok) load(true, t0);
+            queries(1);
+            ++n_items;
+            for (int u = t0 + 1; u < t1 && ok; ++u) {
+                load(false, u);
+                if (ok) load(true, u);
             }
             more = walk.next(it);
         }
@@ -254,40 +225,36 @@ prefill_umma_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_con
             // something timed out: wait (bounded) for the loads in flight before shared memory is given up
             for (uint32_t i = filled > STAGES ? filled - STAGES : 0; i < filled; ++i)
                 mbar_wait_slow(bar(kBarFull + i % STAGES), (i / STAGES) & 1u, nullptr, p.status, limit / 4 + 1);
-            if (n_items > 0) mbar_wait_slow(bar(kBarQFull), static_cast<uint32_t>(n_items - 1) & 1u, nullptr, p.status, limit / 4 + 1);
+            for (int L = 0; L < 2 && n_items > 0; ++L)
+                mbar_wait_slow(bar(kBarQFull + L), static_cast<uint32_t>(n_items - 1) & 1u, nullptr, p.status, limit / 4 + 1);
         }
-    } else if (warp == kMmaWarp || warp == kMmaWarp + 1) {
-        // ------------------------------------------------------------------ products of one lane
-        const int L = warp - kMmaWarp;
+    } else if (warp == kMmaWarp) {
+        // ------------------------------------------------------------------ products of both lanes
+        // One warp issues them all, lane 0's PV(u) QK(u + 1) and then lane 1's: the tensor pipe takes them in this order, which
+        // keeps the lanes half a step apart.  It takes few instructions ahead, so whatever this warp does between them is
+        // time in which the pipe stands still.
         uint32_t elected;
         asm volatile("{\n\t.reg .pred P;\n\telect.sync _|P, 0xFFFFFFFF;\n\tselp.b32 %0, 1, 0, P;\n\t}" : "=r"(elected));
-        uint32_t stage_next = 0, phase_next = 0, p_count = 0;
+        uint32_t stage = 0, phase = 0, p_count[2] = {0, 0};
         auto wait = [&](uint32_t b, uint32_t parity) {
             if (!__all_sync(0xFFFFFFFFu, mbar_try(b, parity)))
                 ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait_slow(b, parity, abort_flag, p.status, limit));
         };
         auto wait_stage = [&]() {
-            const uint32_t stage = stage_next;
-            wait(bar(kBarFull + stage), phase_next);
-            if (++stage_next == STAGES) {
-                stage_next = 0;
-                phase_next ^= 1u;
+            const uint32_t now = stage;
+            wait(bar(kBarFull + stage), phase);
+            if (++stage == STAGES) {
+                stage = 0;
+                phase ^= 1u;
             }
-            return stage;
+            return now;
         };
-        const uint64_t q_desc = smem_desc(q_u32 + static_cast<uint32_t>(L) * Cfg::kQBytes, 16, 1024), k_desc = smem_desc(kv_u32, 16, 1024),
-                       v_desc = smem_desc(kv_u32, kHalfBytes, 1024);
-        const uint32_t t_s = tmem + static_cast<uint32_t>(L) * 256u, t_o = t_s + 128u;
-        // Every stage is waited for and handed back, used or not: a wait tells a phase from its neighbours only.
-        auto pass = [&](uint32_t stage) {
-            if (elected && ok) mbar_arrive(bar(kBarEmpty + stage));
-            __syncwarp();
-        };
+        const uint64_t q_desc = smem_desc(q_u32, 16, 1024), k_desc = smem_desc(kv_u32, 16, 1024), v_desc = smem_desc(kv_u32, kHalfBytes, 1024);
         // value rows between a tile's last key and the next multiple of 16: whatever the slab holds there, and 0 times
-        // a NaN would not be 0 (both lanes' warps may do it: they write the same)
-        auto clear_tail = [&](int keys, uint32_t stage) {
+        // a NaN would not be 0
+        auto clear_tail = [&](int keys, uint32_t at) {
             const int end = (keys + 15) & ~15;
-            uint8_t* vb = kv + stage * Cfg::kStageBytes;
+            uint8_t* vb = kv + at * Cfg::kStageBytes;
             for (int i = lane; i < (end - keys) * 8 * Cfg::kHalves; i += 32) {
                 const int row = keys + i / (8 * Cfg::kHalves), c = i % (8 * Cfg::kHalves);
                 *reinterpret_cast<uint4*>(vb + (c >> 3) * kHalfBytes + row * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
@@ -295,81 +262,134 @@ prefill_umma_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_con
             fence_proxy_async();
             __syncwarp();
         };
-        for (int n_items = 0; ok; ++n_items) {
+        // What the products need to know of an item.
+        struct Work {
+            int steps, k0, tile_keys;                    // steps, the first one's first key, keys that the tile's last token sees
+            int own[2], keys[2];                         // of each lane
+        };
+        int n_items = 0;
+        auto next_item = [&](Work& w) {                  // steps = 0: there is none
             const int slot = n_items & (kItemSlots - 1);
             wait(bar(kBarItem + slot), static_cast<uint32_t>(n_items / kItemSlots) & 1u);
-            if (!ok) break;
-            const PrefillItem it = items[slot];
-            if (it.t1 == 0) break;
-            const int own = lane_steps(it, L), steps = it.t1 - it.t0;
-            const int lane_keys = lane_end(it, L), tile_keys = it.ctx + min(it.tok0 + 2 * lane_tokens, it.add);
-            wait(bar(kBarQFull), static_cast<uint32_t>(n_items) & 1u);
-            if (own == 0) {
-                if (elected && ok) mbar_arrive(bar(kBarQFree));
-                __syncwarp();
+            ++n_items;
+            w.steps = 0;
+            if (!ok) return;
+            const PrefillItem& it = items[slot];
+            w.steps = it.t1 == 0 ? 0 : it.t1 - it.t0;
+            w.k0 = it.t0 * kStep;
+#pragma unroll
+            for (int L = 0; L < 2; ++L) {
+                w.own[L] = lane_steps(it, L);
+                w.keys[L] = lane_end(it, L);
             }
-            auto first = [&](int u) {                    // S of step u; the keys' stage is handed back, and after the last the queries
-                const uint32_t stage = wait_stage();
+            w.tile_keys = max(w.keys[0], w.keys[1]);
+        };
+        // S of lane L
+        auto scores = [&](int L, uint32_t at) {
+            const uint64_t qd = q_desc + static_cast<uint32_t>(L) * (Cfg::kQBytes >> 4), kd = k_desc + at * (Cfg::kStageBytes >> 4);
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+                umma_ss(elected, tmem + static_cast<uint32_t>(L) * 256u, qd + (((k >> 2) * kHalfBytes + (k & 3) * 32) >> 4),
+                        kd + (((k >> 2) * kHalfBytes + (k & 3) * 32) >> 4), IDESC_QK, k > 0 ? 1u : 0u);
+            commit(elected, bar(kBarS + L));
+        };
+        // The same for step u of an item; after its last the queries are handed back
+        auto first = [&](int L, const Work& w, int u, uint32_t at) {
+            if (u == 0) {
+                wait(bar(kBarQFull + L), static_cast<uint32_t>(n_items - 1) & 1u);
                 if (!ok) return;
-                if (u >= own) {
-                    pass(stage);
-                    return;
-                }
-                const uint64_t kd = k_desc + stage * (Cfg::kStageBytes >> 4);
                 tc_fence_after();
-#pragma unroll
-                for (int ks = 0; ks < D / 16; ++ks)
-                    umma_ss(elected, t_s, q_desc + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4), kd + (((ks >> 2) * kHalfBytes + (ks & 3) * 32) >> 4),
-                            IDESC_QK, ks > 0 ? 1u : 0u);
-                commit(elected, bar(kBarS + L));
-                commit(elected, bar(kBarEmpty + stage));
-                if (u + 1 == own) commit(elected, bar(kBarQFree));
-            };
-            first(0);
-            for (int u = 0; u < steps && ok; ++u) {
-                const uint32_t vs = wait_stage();
-                if (!ok) break;
-                if (u < own) {
-                    const int k0 = (it.t0 + u) * kStep;
-                    const int slices = (min(kStep, lane_keys - k0) + 15) >> 4;           // of 16 keys
-                    if (tile_keys - k0 < slices * 16) clear_tail(tile_keys - k0, vs);
-                    const uint64_t vd = v_desc + vs * (Cfg::kStageBytes >> 4);
-                    auto product = [&](int ks) {
-                        umma_ts(elected, t_o, t_s + static_cast<uint32_t>(ks * 8), vd + ((ks * 2048) >> 4), IDESC_PV, (u == 0 && ks == 0) ? 0u : 1u);
-                    };
-                    wait(bar(kBarPa + L), p_count & 1u);
-                    if (!ok) break;
-                    tc_fence_after();
-                    if (slices >= 4) {
-#pragma unroll
-                        for (int ks = 0; ks < 4; ++ks) product(ks);
-                    } else {
-                        for (int ks = 0; ks < slices; ++ks) product(ks);
-                    }
-                    commit(elected, bar(kBarHalf + L));
-                    wait(bar(kBarPb + L), p_count & 1u);
-                    if (!ok) break;
-                    tc_fence_after();
-                    if (slices == 8) {
-#pragma unroll
-                        for (int ks = 4; ks < 8; ++ks) product(ks);
-                    } else {
-                        for (int ks = 4; ks < slices; ++ks) product(ks);
-                    }
-                    ++p_count;
-                    commit(elected, bar(kBarEmpty + vs));
-                    if (u + 1 == own) commit(elected, bar(kBarO + L));
-                } else {
-                    pass(vs);
-                }
-                if (u + 1 < steps) first(u + 1);
             }
+            if (u < w.own[L]) scores(L, at);
+            if (u == max(w.own[L] - 1, 0)) commit(elected, bar(kBarQFree + L));
+        };
+        // O of lane L += P V of step u.  INNER: not the lane's last step, nor the tile's first.
+        auto second = [&](auto inner, int L, const Work& w, int u, uint32_t at) {
+            constexpr bool INNER = decltype(inner)::value;
+            const uint32_t t_s = tmem + static_cast<uint32_t>(L) * 256u, t_o = t_s + 128u;
+            const uint64_t vd = v_desc + at * (Cfg::kStageBytes >> 4);
+            auto product = [&](int k) {                  // 16 keys
+                umma_ts(elected, t_o, t_s + static_cast<uint32_t>(k * 8), vd + ((k * 2048) >> 4), IDESC_PV, (!INNER && u == 0 && k == 0) ? 0u : 1u);
+            };
+            const bool full = INNER || u + 1 < w.own[L];
+            int slices = 8;
+            wait(bar(kBarPa + L), p_count[L] & 1u);
+            if (!ok) return;
+            tc_fence_after();
+            if (!full) {                                 // the lane's last step: as many keys as there are
+                const int k0 = w.k0 + u * kStep;
+                slices = (min(kStep, w.keys[L] - k0) + 15) >> 4;
+                if (w.tile_keys - k0 < kStep) clear_tail(w.tile_keys - k0, at);
+            }
+            auto products = [&](int from) {
+                if (slices >= from + 4) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) product(from + k);
+                } else {
+                    for (int k = from; k < slices; ++k) product(k);
+                }
+            };
+            products(0);
+            commit(elected, bar(kBarHalf + L));
+            wait(bar(kBarPb + L), p_count[L] & 1u);
+            if (!ok) return;
+            tc_fence_after();
+            products(4);
+            ++p_count[L];
+            if (!full) commit(elected, bar(kBarO + L));
+        };
+        // The steps of all items in one sequence, a lane's PV of one and QK of the next at a time: the end of a tile for
+        // one lane is under way beside the other's.  Both stages are waited for ahead of the weights: between a lane's two
+        // products the tensor pipe would idle.
+        Work now, next;
+        next_item(now);
+        if (ok && now.steps > 0) {
+            const uint32_t ks = wait_stage();
+            if (ok) first(0, now, 0, ks);
+            if (ok) first(1, now, 0, ks);
+            commit(elected, bar(kBarEmpty + ks));
+        }
+        for (int u = 0; ok && now.steps > 0;) {
+            const int inner = min(now.own[0], now.own[1]) - 2;       // both lanes have this step, the next, and one more
+            while (u > 0 && u < inner) {
+                const uint32_t vs = wait_stage(), ks = wait_stage();
+                if (!ok) break;
+                second(std::true_type(), 0, now, u, vs);
+                if (!ok) break;
+                scores(0, ks);
+                second(std::true_type(), 1, now, u, vs);
+                if (!ok) break;
+                commit(elected, bar(kBarEmpty + vs));
+                scores(1, ks);
+                commit(elected, bar(kBarEmpty + ks));
+                ++u;
+            }
+            if (!ok) break;
+            const bool last = u + 1 == now.steps;
+            next = now;
+            if (last) next_item(next);
+            const int v = last ? 0 : u + 1;              // the next step
+            const uint32_t vs = wait_stage();
+            uint32_t ks = 0;
+            if (next.steps > 0) ks = wait_stage();
+            if (!ok) break;
+            if (u < now.own[0]) second(std::false_type(), 0, now, u, vs);
+            if (ok && next.steps > 0) first(0, next, v, ks);
+            if (ok && u < now.own[1]) second(std::false_type(), 1, now, u, vs);
+            if (!ok) break;
+            commit(elected, bar(kBarEmpty + vs));
+            if (next.steps > 0) {
+                first(1, next, v, ks);
+                commit(elected, bar(kBarEmpty + ks));
+            }
+            now = next;
+            u = v;
         }
         // nothing may still be running when tensor memory is given back
-        commit(elected, bar(kBarDrain + L));
+        commit(elected, bar(kBarDrain));
         __syncwarp();
-        mbar_wait_slow(bar(kBarDrain + L), 0, nullptr, p.status, limit / 4 + 1);
-    } else if (warp < 8) {
+        mbar_wait_slow(bar(kBarDrain), 0, nullptr, p.status, limit / 4 + 1);
+    } else if (warp < kSoftmaxWarps) {
         // ------------------------------------------------------------------ softmax
         const int L = warp >> 2;
         const int row = (warp & 3) * 32 + lane;          // of the lane's tile
@@ -383,89 +403,129 @@ prefill_umma_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_con
             if (!ok) break;
             const PrefillItem it = items[slot];
             if (it.t1 == 0) break;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(kBarQFree + L));          // the slot has been read
+            __syncwarp();
             const int own = lane_steps(it, L);
             const int tok = it.tok0 + L * lane_tokens + row_tok;
             const int sees = it.ctx + min(tok, it.add - 1) + 1;                  // keys of this row
             const int all_see = it.ctx + it.tok0 + L * lane_tokens + 1;          // keys of the lane's first row
+            const int2 warp_sees = make_int2(__shfl_sync(0xFFFFFFFFu, sees, 0), __shfl_sync(0xFFFFFFFFu, sees, 31));     // of the warp's first and last
             float m = -INFINITY, l = 0.f;                // reference (log2 units) and sum
-            float most = NAN;                            // a maximum above it raises the reference (no reference yet: any)
             for (int u = 0; u < own && ok; ++u) {
                 ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(kBarS + L), s_count & 1u, abort_flag, p.status, limit));
                 if (!ok) break;
                 tc_fence_after();
                 const int k0 = (it.t0 + u) * kStep;
-                // The reference of the warp's rows goes up: what has been computed with the one before is scaled.  `c`: chunks of
-                // this step already in P; `o`: O holds something.
-                auto raise = [&](float top, int c, bool o) {
-                    const bool up = m == -INFINITY ? top > m : top > most;
+                const bool masked = k0 + kStep > all_see;            // some row of the lane does not see all of the step
+                // The reference of the warp's rows goes up to `top` where that is higher: O and the sum, computed with the one
+                // before, are scaled.  `half`: of this step, whose first product may be under way when the second raises it.
+                auto raise = [&](float top, int half) {
                     const float before = m;
-                    if (up) {
-                        m = top;
-                        most = top + kRescaleAbove;
-                    }
-                    const float f = up ? fast_exp2(before - m) : 1.f;
+                    if (top > m) m = top;
+                    const float f = top > before ? fast_exp2(before - m) : 1.f;
                     l *= f;
-                    if (c >= 2 && ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(kBarHalf + L), s_count & 1u, abort_flag, p.status, limit));
+                    if (half == 0 && u == 0) return;     // nothing in O yet
+                    if (half == 1) ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(kBarHalf + L), s_count & 1u, abort_flag, p.status, limit));
                     if (!ok) return;
                     tc_fence_after();
-                    if (o || c >= 2) {
 #pragma unroll 1
-                        for (int k = 0; k < D / 16; ++k) {
-                            uint32_t v[16];
-                            tmem_ld_row16(t_o + 16u * k, v);
-                            tmem_wait_ld();
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
-                            tmem_st_row16(t_o + 16u * k, v);
-                        }
-                    }
-                    if (c & 1) {                         // the first chunk of this half
+                    for (int k = 0; k < D / 16; ++k) {
                         uint32_t v[16];
-                        tmem_ld_row16(t_s + 16u * (c - 1), v);
+                        tmem_ld_row16(t_o + 16u * k, v);
                         tmem_wait_ld();
 #pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            v[i] = pack_bf16(__uint_as_float(v[i] << 16) * f, __uint_as_float(v[i] & 0xFFFF0000u) * f);
-                        tmem_st_row16(t_s + 16u * (c - 1), v);
+                        for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
+                        tmem_st_row16(t_o + 16u * k, v);
                     }
                     tmem_wait_st();
                 };
-                auto step = [&](auto masked) {
-                    constexpr bool MASK = decltype(masked)::value;
+                auto chunk = [&](uint32_t(&x)[kChunk], int c) {      // 32 scores, those of keys that the row does not see -inf
+                    tmem_ld_row32(t_s + static_cast<uint32_t>(c * kChunk), x);
+                    tmem_wait_row32(x);
+                    if (k0 + (c + 1) * kChunk > warp_sees.x) {
+                        const int keys = sees - k0 - c * kChunk;
+                        const uint32_t in = keys >= kChunk ? 0xFFFFFFFFu : keys <= 0 ? 0u : (1u << keys) - 1u;
+#pragma unroll
+                        for (int i = 0; i < kChunk; ++i)
+                            if (!(in >> i & 1u)) x[i] = 0xFF800000u;
+                    }
+                };
+                auto hand_over = [&](int half) {
+                    tmem_wait_st();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar((half == 0 ? kBarPa : kBarPb) + L));
+                    __syncwarp();                        // the loads and stores of tensor memory want the whole warp
+                };
+                if (u == 0 || masked) {                  // the maximum first: there may be no reference yet
+                    float top = -INFINITY;
+#pragma unroll 1
+                    for (int c = 0; c < kStep / kChunk; ++c) {
+                        if (k0 + c * kChunk >= warp_sees.y) break;
+                        uint32_t x[kChunk];
+                        chunk(x, c);
+                        top = fmaxf(top, row_max(x));
+                    }
+                    top *= scale;
+                    if (__any_sync(0xFFFFFFFFu, top > m + kRaiseAbove || (m == -INFINITY && top > m))) raise(top, 0);
+                    if (!ok) break;
+                }
+                if (masked) {
+#pragma unroll 1
+                    for (int c = 0; c < kStep / kChunk; ++c) {
+                        uint32_t pk[kChunk / 2];
+                        if (k0 + c * kChunk < warp_sees.y) {
+                            uint32_t x[kChunk];
+                            chunk(x, c);
+                            l += weights(x, scale, m == -INFINITY ? 0.f : m, pk);
+                        } else {                         // nobody sees any of it
+#pragma unroll
+                            for (int i = 0; i < kChunk / 2; ++i) pk[i] = 0u;
+                        }
+                        tmem_st_row16(t_s + 16u * c, pk);
+                        if (c & 1) hand_over(c >> 1);
+                    }
+                } else {
                     uint32_t s[2][kChunk];
                     tmem_ld_row32(t_s, s[0]);
 #pragma unroll
-                    for (int c = 0; c < kStep / kChunk; ++c) {
-                        uint32_t(&x)[kChunk] = s[c & 1];
-                        tmem_wait_row32(x);
-                        if (c + 1 < kStep / kChunk) tmem_ld_row32(t_s + static_cast<uint32_t>((c + 1) * kChunk), s[(c + 1) & 1]);
-                        if (MASK) {
-                            const int keys = sees - k0 - c * kChunk;
+                    for (int half = 0; half < 2; ++half) {
+                        uint32_t pk[2][kChunk / 2];
+                        float sum = 0.f;
+                        const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
-                            for (int i = 0; i < kChunk; ++i)
-                                if (i >= keys) x[i] = 0xFF800000u;       // -inf
+                        for (int k = 0; k < 2; ++k) {
+                            const int c = 2 * half + k;
+                            tmem_wait_row32(s[k]);
+                            if (c < 3) tmem_ld_row32(t_s + static_cast<uint32_t>((c + 1) * kChunk), s[k ^ 1]);
+                            sum += weights(s[k], scale, ref, pk[k]);
                         }
-                        uint32_t pk[kChunk / 2];
-                        float sum = weights<MASK ? 0 : kPolyPairs>(x, scale, m == -INFINITY ? 0.f : m, pk);
-                        const float top = row_max(x) * scale;
-                        if (__any_sync(0xFFFFFFFFu, !(top <= most))) {
-                            raise(top, c, u > 0);
-                            sum = weights<0>(x, scale, m == -INFINITY ? 0.f : m, pk);
+                        // no reference yet, or one that is too low (or a NaN, which stays)
+                        if (__any_sync(0xFFFFFFFFu, m == -INFINITY || !(sum <= kTooLarge))) {
+                            float top = -INFINITY;
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                uint32_t x[kChunk];      // again from tensor memory, where P has not come yet
+                                chunk(x, 2 * half + k);
+                                top = fmaxf(top, row_max(x));
+                            }
+                            raise(top * scale, half);
+                            const float up = m == -INFINITY ? 0.f : m;
+                            sum = 0.f;
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                uint32_t x[kChunk];
+                                chunk(x, 2 * half + k);
+                                sum += weights(x, scale, up, pk[k]);
+                            }
                         }
                         l += sum;
-                        tmem_st_row16(t_s + 16u * c, pk);
-                        if (c == 1 || c == 3) {
-                            tmem_wait_st();
-                            tc_fence_before();
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(bar((c == 1 ? kBarPa : kBarPb) + L));
-                        }
+                        tmem_st_row16(t_s + 32u * half, pk[0]);
+                        tmem_st_row16(t_s + 32u * half + 16u, pk[1]);
+                        hand_over(half);
                     }
-                };
-                if (k0 + kStep <= all_see)
-                    step(std::false_type());
-                else
-                    step(std::true_type());
+                }
                 ++s_count;
             }
             if (!ok) break;
@@ -477,7 +537,7 @@ prefill_umma_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_con
                 tc_fence_after();
             }
             const bool mine = row < lane_rows && tok < it.add;
-            const float inv = it.slot >= 0 ? 1.f : p.v_scale / l;
+            const float inv = p.v_scale / l;
             const int64_t out_row = static_cast<int64_t>(it.cu + tok) * p.q_heads + it.head * p.group + row_head;
             const int64_t part_row = static_cast<int64_t>(it.slot) * p.part_rows + L * lane_rows + row;
 #pragma unroll 1
