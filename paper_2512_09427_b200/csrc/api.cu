@@ -1384,7 +1384,7 @@ bool prefill_shape(const odma_pool* pool, int32_t q_heads, const odma_tables* t,
     if (!pool || !t || t->n < 1 || t->n > kMaxPrefillBatch || t->n_new_total < 0 || q_heads < pool->kv_heads || q_heads % pool->kv_heads != 0)
         return false;
     const int32_t group = q_heads / pool->kv_heads, D = pool->head_dim;
-    if (group > kMaxPrefillGroup || group > pool->alloc.config().max_group || (D != 32 && D != 64 && D != 128)) return false;
+    if (pool->plan_ctas > kMaxDeviceCtas || group > kMaxPrefillGroup || group > pool->alloc.config().max_group || (D != 32 && D != 64 && D != 128)) return false;
     PrefillShape w;
     w.tensor = pool->dtype != ODMA_DTYPE_F32 && D != 32;
     w.tile_tokens = w.tensor ? 2 * (kPrefillRows / 2 / group) : kPrefillPlainRows / group;

@@ -205,9 +205,12 @@ cudaError_t launch_plain_t(const PrefillParams& p, cudaStream_t stream) {
 
 // ---- 8-bit pools
 
-// A block column per request with new tokens: rows [0, len) of every head, K and V, to the place that the plan gives them.
+// Rows [0, len) of every head, K and V, of the requests with new tokens to the place that the plan gives them: blockIdx.y the
+// request, blockIdx.z the array and head; a thread takes kWiden vectors of 16 codes, all loads before the first store.
+constexpr int kWiden = 4;
 __global__ void __launch_bounds__(256) prefill_widen_kernel(const PrefillParams p) {
     __shared__ int64_t sums[8];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int i = blockIdx.y, len = __ldg(p.len + i), D = p.head_dim;
     if (prefill_new(p, i, len) == 0) return;
     int64_t before = 0;                              // tokens of the requests ahead
@@ -227,17 +230,21 @@ __global__ void __launch_bounds__(256) prefill_widen_kernel(const PrefillParams 
         if (blockIdx.x == 0 && threadIdx.x == 0) atomicOr(p.status, kStatusOverflow);
         return;
     }
+    const int h = blockIdx.z >> 1, is_v = blockIdx.z & 1;
     const int64_t vecs = static_cast<int64_t>(len) * D / 16, step = static_cast<int64_t>(gridDim.x) * 256;
     const int64_t slab = static_cast<int64_t>(__ldg(p.base + i)) * p.kv_heads, cap = __ldg(p.cap + i);
-    const uint8_t* pool = static_cast<const uint8_t*>(p.pool);
-    for (int a = 0; a < 2 * p.kv_heads; ++a) {
-        const int h = a >> 1;
-        const uint4* src = reinterpret_cast<const uint4*>(pool + ((a & 1 ? p.v_row0 : p.k_row0) + slab + h * cap) * D);
-        uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.wide) +
-                                              (((a & 1) * p.wide_tokens + before) * p.kv_heads + static_cast<int64_t>(h) * pad) * D);
-        for (int64_t v = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; v < vecs; v += step) {
-            const uint4 c = __ldg(src + v);
-            const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+    const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(p.pool) + ((is_v ? p.v_row0 : p.k_row0) + slab + h * cap) * D);
+    uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.wide) +
+                                          ((is_v * p.wide_tokens + before) * p.kv_heads + static_cast<int64_t>(h) * pad) * D);
+    for (int64_t v = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; v < vecs; v += kWiden * step) {
+        uint4 c[kWiden];
+#pragma unroll
+        for (int u = 0; u < kWiden; ++u)
+            if (v + u * step < vecs) c[u] = __ldg(src + v + u * step);
+#pragma unroll
+        for (int u = 0; u < kWiden; ++u) {
+            if (v + u * step >= vecs) break;
+            const uint32_t w[4] = {c[u].x, c[u].y, c[u].z, c[u].w};
             uint32_t o[8];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -245,8 +252,9 @@ __global__ void __launch_bounds__(256) prefill_widen_kernel(const PrefillParams 
                 o[2 * j] = pack_bf16(lo.x, lo.y);
                 o[2 * j + 1] = pack_bf16(hi.x, hi.y);
             }
-            dst[2 * v] = make_uint4(o[0], o[1], o[2], o[3]);
-            dst[2 * v + 1] = make_uint4(o[4], o[5], o[6], o[7]);
+            uint4* to = dst + 2 * (v + u * step);
+            to[0] = make_uint4(o[0], o[1], o[2], o[3]);
+            to[1] = make_uint4(o[4], o[5], o[6], o[7]);
         }
     }
 }
@@ -257,94 +265,101 @@ constexpr int kMergeWarps = 8;
 
 __device__ __forceinline__ bool same_tile(const int4& a, const int4& b) { return a.x == b.x && a.y == b.y && a.z == b.z; }
 
-// Block (s, y): if share s begins inside a tile and is the first to do so, the tile's pieces are those of shares s - 1
-// (its last), s, s + 1, ... up to the one that ends the tile; a warp takes a row.
-template <typename T, int V>        // head_dim = 32 * V
-__global__ void __launch_bounds__(kMergeWarps * 32) prefill_merge_kernel(const PrefillParams p) {
-    constexpr int D = 32 * V;
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int s = static_cast<int>(blockIdx.x) + 1, lane = threadIdx.x & 31;
-    const int4 c = __ldcg(p.starts + s);
-    if (c.w == 0 || c.x >= p.n) return;
-    const int4 ahead = __ldcg(p.starts + s - 1);
-    if (ahead.w > 0 && same_tile(ahead, c)) return;
-    const int len = __ldg(p.len + c.x), add = prefill_new(p, c.x, len), tok0 = c.z * p.tile_tokens;
-    const int rows = min(p.tile_tokens, add - tok0) * p.group;
-    const int first = blockIdx.y * kMergeWarps + (threadIdx.x >> 5);
-    if (first >= rows) return;
-    // shares s .. s + more - 1 hold a piece that begins behind a cut (an empty one, between two equal cuts, none)
-    int more = 1;
-    for (; s + more < p.shares; more += 32) {
-        const int k = s + more + lane;
-        const int4 x = k < p.shares ? __ldcg(p.starts + k) : make_int4(-1, 0, 0, 0);
-        const uint32_t in = __ballot_sync(0xFFFFFFFFu, x.w > 0 && same_tile(x, c));
-        if (in != 0xFFFFFFFFu) {
-            more += __ffs(~in) - 1;
-            break;
+template <int V>
+struct RowPart {
+    float2 ml;
+    float x[V];
+    __device__ __forceinline__ void load(const PrefillParams& p, int64_t at, int lane) {
+        ml = __ldcg(reinterpret_cast<const float2*>(p.part_ml + 2 * at));
+        const float* from = p.part_o + (at * 32 + lane) * V;
+        if constexpr (V == 4) {
+            const float4 v = ldcg4(from);
+            x[0] = v.x, x[1] = v.y, x[2] = v.z, x[3] = v.w;
+        } else if constexpr (V == 2) {
+            const float2 v = __ldcg(reinterpret_cast<const float2*>(from));
+            x[0] = v.x, x[1] = v.y;
+        } else {
+            x[0] = __ldcg(from);
         }
     }
-    more = min(more, p.shares - s);
-    for (int r = first; r < rows; r += gridDim.y * kMergeWarps) {
+};
+
+// The rows of all cut tiles, dealt to the warps of the grid; a warp takes a row, kUnder pieces under way at a time.  If share s
+// begins inside a tile and is the first to do so, the tile's pieces are those of share s - 1 (its last), s, s + 1, ... up to
+// the one that ends the tile.  Launched programmatically: a block is there when the kernel ahead ends.
+template <typename T, int V>        // head_dim = 32 * V
+__global__ void __launch_bounds__(kMergeWarps * 32) prefill_merge_kernel(const PrefillParams p) {
+    constexpr int kUnder = 4;
+    extern __shared__ int4 start[];                  // [shares + 1]
+    int32_t* tile = reinterpret_cast<int32_t*>(start + p.shares + 1);        // shares that are the first to cut their tile
+    __shared__ int tiles;
+    const int tid = threadIdx.x, lane = tid & 31;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    for (int i = tid; i <= p.shares; i += kMergeWarps * 32) start[i] = __ldcg(p.starts + i);
+    __syncthreads();
+    if (tid < 32) {
+        int n = 0;
+        for (int s0 = 1; s0 < p.shares; s0 += 32) {
+            const int s = s0 + lane;
+            bool cut = s < p.shares && start[s].w > 0 && start[s].x < p.n;
+            cut = cut && !(start[s - 1].w > 0 && same_tile(start[s - 1], start[s]));
+            const uint32_t all = __ballot_sync(0xFFFFFFFFu, cut);
+            if (cut) tile[n + __popc(all & ((1u << lane) - 1u))] = s;
+            n += __popc(all);
+        }
+        if (lane == 0) tiles = n;
+    }
+    __syncthreads();
+    const int work = tiles * p.part_rows;
+    for (int i = static_cast<int>(blockIdx.x) * kMergeWarps + (tid >> 5); i < work; i += static_cast<int>(gridDim.x) * kMergeWarps) {
+        const int s = tile[i / p.part_rows], r = i % p.part_rows;
+        const int4 c = start[s];
+        const int add = prefill_new(p, c.x, __ldg(p.len + c.x)), tok0 = c.z * p.tile_tokens, cu = __ldg(p.cu_new + c.x);
+        if (r >= min(p.tile_tokens, add - tok0) * p.group) continue;
         float M = -INFINITY, L = 0.f, acc[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) acc[i] = 0.f;
-        for (int k0 = 0; k0 <= more; k0 += 32) {     // piece 0: of share s - 1
-            const int k = k0 + lane;
-            int64_t at = -1;
-            if (k == 0) {
-                at = static_cast<int64_t>(2 * (s - 1) + 1) * p.part_rows + r;
-            } else if (k <= more) {
-                const int4 a = __ldcg(p.starts + s + k - 1), b = __ldcg(p.starts + s + k);
-                if (!(same_tile(a, b) && a.w == b.w)) at = static_cast<int64_t>(2 * (s + k - 1)) * p.part_rows + r;
-            }
-            float2 ml = make_float2(-INFINITY, 0.f);
-            if (at >= 0) ml = __ldcg(reinterpret_cast<const float2*>(p.part_ml + 2 * at));
-            float top = M;
-            bool bad = ml.x != ml.x;                 // a NaN among the scores stays one
-            top = fmaxf(top, ml.x);
+        for (int k = 0; k < V; ++k) acc[k] = 0.f;
+        bool more = true;
+        for (int k0 = 0; more; k0 += 32) {           // piece 0: of share s - 1
+            const int k = s + k0 + lane;             // the share behind the piece's
+            // (an empty share, between two equal cuts, has none)
+            const bool in = k <= p.shares && (k == s || (k - 1 < p.shares && start[k - 1].w > 0 && same_tile(start[k - 1], c)));
+            const bool none = in && k > s && same_tile(start[k - 1], start[k]) && start[k - 1].w == start[k].w;
+            const int slot = !in || none ? -1 : k == s ? 2 * s - 1 : 2 * (k - 1);
+            const uint32_t all = __ballot_sync(0xFFFFFFFFu, in);
+            more = all == 0xFFFFFFFFu;
+            const int count = more ? 32 : __ffs(~all) - 1;
+            for (int j0 = 0; j0 < count; j0 += kUnder) {
+                RowPart<V> part[kUnder];
+                int from[kUnder];
 #pragma unroll
-            for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, d));
-            const float e = ml.x == -INFINITY ? 0.f : bad ? NAN : fast_exp2(ml.x - top), old = M == -INFINITY ? 0.f : fast_exp2(M - top);
-            float sum = ml.x == -INFINITY ? 0.f : ml.y * e;
-#pragma unroll
-            for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d);
-            L = fmaf(L, old, sum);
-            M = top;
-#pragma unroll
-            for (int i = 0; i < V; ++i) acc[i] *= old;
-            const int count = min(32, more + 1 - k0);
-            for (int j = 0; j < count; ++j) {
-                const float w = __shfl_sync(0xFFFFFFFFu, e, j);
-                const int64_t from = __shfl_sync(0xFFFFFFFFu, at, j);
-                if (w == 0.f) continue;              // no key of the piece is seen by the row
-                float x[V];
-                if constexpr (V == 4) {
-                    const float4 v = ldcg4(p.part_o + from * D + lane * 4);
-                    x[0] = v.x;
-                    x[1] = v.y;
-                    x[2] = v.z;
-                    x[3] = v.w;
-                } else if constexpr (V == 2) {
-                    const float2 v = __ldcg(reinterpret_cast<const float2*>(p.part_o + from * D + lane * 2));
-                    x[0] = v.x;
-                    x[1] = v.y;
-                } else {
-                    x[0] = __ldcg(p.part_o + from * D + lane);
+                for (int j = 0; j < kUnder; ++j) {
+                    from[j] = __shfl_sync(0xFFFFFFFFu, slot, (j0 + j) & 31);
+                    if (j0 + j >= count) from[j] = -1;
+                    if (from[j] >= 0) part[j].load(p, static_cast<int64_t>(from[j]) * p.part_rows + r, lane);
                 }
 #pragma unroll
-                for (int i = 0; i < V; ++i) acc[i] = fmaf(x[i], w, acc[i]);
+                for (int j = 0; j < kUnder; ++j) {
+                    if (from[j] < 0 || part[j].ml.y == 0.f) continue;    // (a piece whose keys the row does not see has no sum)
+                    const float top = fmaxf(M, part[j].ml.x);
+                    const float a = M == -INFINITY ? 0.f : fast_exp2(M - top), b = part[j].ml.x == -INFINITY ? 1.f : fast_exp2(part[j].ml.x - top);
+                    L = fmaf(L, a, part[j].ml.y * b);
+                    M = top;
+#pragma unroll
+                    for (int e = 0; e < V; ++e) acc[e] = fmaf(acc[e], a, part[j].x[e] * b);
+                }
             }
         }
         const float inv = p.v_scale / L;
-        const int64_t row = static_cast<int64_t>(__ldg(p.cu_new + c.x) + tok0 + r / p.group) * p.q_heads + c.y * p.group + r % p.group;
-        T* to = static_cast<T*>(p.out) + row * D + lane * V;
+        const int64_t row = static_cast<int64_t>(cu + tok0 + r / p.group) * p.q_heads + c.y * p.group + r % p.group;
+        T* to = static_cast<T*>(p.out) + (row * 32 + lane) * V;
 #pragma unroll
-        for (int i = 0; i < V; ++i) acc[i] *= inv;
+        for (int k = 0; k < V; ++k) acc[k] *= inv;
         if constexpr (V == 4)
             store4(to, acc[0], acc[1], acc[2], acc[3]);
         else
 #pragma unroll
-            for (int i = 0; i < V; ++i) to[i] = static_cast<T>(acc[i]);
+            for (int k = 0; k < V; ++k) to[k] = static_cast<T>(acc[k]);
         if (lane == 0 && p.lse) p.lse[row] = (M + log2f(L)) * 0.6931471805599453f;
     }
 }
@@ -353,8 +368,9 @@ template <typename T, int V>
 cudaError_t launch_merge_t(const PrefillParams& p, cudaStream_t stream) {
     if (p.shares < 2) return cudaSuccess;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(static_cast<unsigned>(p.shares - 1), static_cast<unsigned>((p.part_rows + kMergeWarps - 1) / kMergeWarps));
+    cfg.gridDim = dim3(static_cast<unsigned>(std::min(4 * p.shares, (p.shares * p.part_rows + kMergeWarps - 1) / kMergeWarps)));
     cfg.blockDim = dim3(kMergeWarps * 32);
+    cfg.dynamicSmemBytes = static_cast<size_t>(p.shares + 1) * 20;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -375,7 +391,9 @@ cudaError_t launch_prefill_plain(const PrefillParams& p, bool fp32, cudaStream_t
 }
 
 cudaError_t launch_prefill_widen(const PrefillParams& p, cudaStream_t stream) {
-    const dim3 grid(static_cast<unsigned>(std::max(1, std::min(256, 1184 / p.n))), static_cast<unsigned>(p.n));
+    // some blocks per SM in all, whatever the number of requests (their lengths are the device's)
+    const int columns = p.n * 2 * p.kv_heads;
+    const dim3 grid(static_cast<unsigned>(std::max(1, std::min(256, 1184 / columns))), static_cast<unsigned>(p.n), static_cast<unsigned>(2 * p.kv_heads));
     prefill_widen_kernel<<<grid, 256, 0, stream>>>(p);
     return cudaGetLastError();
 }

@@ -122,6 +122,7 @@ prefill_umma_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_con
 
     // ---- set-up: barriers, tensor memory, query rows that no token has, the share
     if (warp == kProducerWarp) {
+        if (lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &kv_map : &q_map) : "memory");
         for (int i = lane; i < kNumBars; i += 32) {
             const bool free = i == kBarQFree || i == kBarQFree + 1;          // a lane's softmax warps; and its last product
             mbar_init(bar(i), free ? 5u : i >= kBarPa && i < kBarHalf ? 4u : 1u);
@@ -140,7 +141,6 @@ prefill_umma_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_con
             *reinterpret_cast<uint4*>(q_lane + (c >> 3) * kHalfBytes + row * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
         }
     }
-    asm volatile("griddepcontrol.wait;" ::: "memory");
     int64_t* cum = reinterpret_cast<int64_t*>(kv + sizeof(PlanScratch));
     int32_t* lens = reinterpret_cast<int32_t*>(cum + p.n);
     prefill_plan<kStep, kThreads>(p, plan, cum, lens, lens + p.n);
@@ -182,6 +182,7 @@ prefill_umma_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_con
             }
         };
         bool more = walk.next(it);
+        asm volatile("griddepcontrol.wait;" ::: "memory");               // 8-bit pools: the kernel ahead writes the rows
         while (ok) {
             // The slot's last item lies four back, and both lanes' softmax warps have read the one two back (they arrive on
             // kBarQFree when they have; the issuing warp is ahead of them).
@@ -595,8 +596,17 @@ cudaError_t launch_t(const CUtensorMap& kv, const CUtensorMap& q, const PrefillP
         if (e != cudaSuccess) return e;
         configured[dev] = true;
     }
-    prefill_umma_kernel<D><<<static_cast<unsigned>(p.shares), kThreads, Config<D>::kSmem, stream>>>(kv, q, p);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(static_cast<unsigned>(p.shares));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = Config<D>::kSmem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = p.wide ? 1 : 0;                    // behind prefill_widen_kernel: set up beside it
+    return cudaLaunchKernelEx(&cfg, prefill_umma_kernel<D>, kv, q, p);
 }
 
 }  // namespace
