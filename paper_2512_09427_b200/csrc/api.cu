@@ -1370,12 +1370,16 @@ namespace {
 // The split and the workspace of a call of odma_prefill_attention.
 struct PrefillShape {
     bool tensor = false;
-    int32_t tile_tokens = 0, part_rows = 0, shares = 0, min_piece = 0;
+    int32_t tile_tokens = 0, part_rows = 0, shares = 0, min_piece = 0, plan_start = 0, plan_cut = 0;
     int64_t wide_tokens = 0;                     // 8-bit pools: tokens widened
     uint64_t wide_bytes = 0, starts_bytes = 0, part_o_bytes = 0, part_ml_bytes = 0;
     uint64_t bytes() const { return wide_bytes + starts_bytes + part_o_bytes + part_ml_bytes; }
 };
 
+// What the plan charges (prefill_plan.cuh), in eighths of a step.  Tensor cores: a tile's beginning and end take as long as
+// 1.1 steps of 128 keys, and its last step is on average half empty; the rows of a cut are as much as six.  Plain ALUs: a step of
+// 64 keys takes 3.7 us, beside which both are small.
+constexpr int32_t kTensorStart = 13, kTensorCut = 48, kPlainStart = 4, kPlainCut = 8;
 // Rows of fewer than 33 queries cost little to write and read again, and one step of 128 keys is worth a cut; a full
 // tile's 256 rows are worth six (prefill_plan.cuh).
 int32_t prefill_min_piece(int32_t rows) { return rows <= 32 ? 1 : rows <= 128 ? 2 : 4; }
@@ -1390,7 +1394,9 @@ bool prefill_shape(const odma_pool* pool, int32_t q_heads, const odma_tables* t,
     w.tile_tokens = w.tensor ? 2 * (kPrefillRows / 2 / group) : kPrefillPlainRows / group;
     w.part_rows = std::max(1, std::min(w.tile_tokens, t->n_new_total)) * group;
     w.shares = w.tensor ? pool->plan_ctas : prefill_plain_blocks() * pool->plan_ctas;
-    w.min_piece = prefill_min_piece(w.part_rows);
+    w.min_piece = w.tensor ? prefill_min_piece(w.part_rows) : 1;
+    w.plan_start = w.tensor ? kTensorStart : kPlainStart;
+    w.plan_cut = w.tensor ? kTensorCut : kPlainCut;
     auto up = [](int64_t b) { return static_cast<uint64_t>((b + 255) / 256 * 256); };
     if (pool->dtype == ODMA_DTYPE_FP8_E4M3) {
         // lengths rounded up to 16; on the device's own lengths all the pool can hold
@@ -1465,6 +1471,8 @@ int32_t odma_prefill_attention(odma_pool* pool, int32_t layer, const void* q, in
     p.part_rows = w.part_rows;
     p.shares = w.shares;
     p.min_piece = w.min_piece;
+    p.plan_start = w.plan_start;
+    p.plan_cut = w.plan_cut;
     p.scale_log2 = d.scale_log2 * d.k_scale;
     p.v_scale = d.v_scale;
     p.status = pool->d_status;

@@ -237,6 +237,7 @@ struct PrefillParams {
     int32_t part_rows;          // rows of a partial result: of a tile, or all there are
     int32_t shares;
     int32_t min_piece;          // steps: a cut closer than this to an end of its tile moves to that end
+    int32_t plan_start, plan_cut;       // eighths of a step: what a tile is charged beside its steps, and a cut
     float scale_log2, v_scale;
     uint32_t* status;
     int64_t wait_limit_ns;

@@ -8,18 +8,15 @@
 //     F(j) = j (c + start) + tile_tokens j (j + 1) / 2
 // and share s of S, which begins at cost s * ceil(total / S), is found by three searches in closed form.  A
 // share that begins inside a tile cuts it: the pieces leave partial results and a second kernel merges them.
-// A cut costs about six steps (its rows are written in 32 bits and read again), so when there are no more
-// tiles than shares and the longest tile ends before an equal share and a cut would, every share takes a
-// tile; and a cut closer than `min_piece` steps to an end of its tile moves to that end.
+// A cut costs some steps too (its rows are written in 32 bits and read again), so when there are no more tiles than shares
+// and the longest tile ends before an equal share and a cut would, every share takes a tile; and a cut closer than
+// `min_piece` steps to an end of its tile moves to that end.
 #pragma once
 
 #include "device_utils.cuh"
 
 namespace odma {
 namespace dev {
-
-constexpr int kPlanStart = 13;      // eighths of a step: what beginning and ending a tile costs, and half a step for its last one
-constexpr int kPlanCut = 48;        // what a cut costs: rows in 32 bits and their merge
 
 struct alignas(16) PlanScratch {                // shared memory of one block
     int64_t sums[3][32];
@@ -40,7 +37,7 @@ __device__ __forceinline__ int prefill_new(const PrefillParams& p, int i, int le
 // whole warp; returns false where the cut moves behind the request.
 template <int STEP>
 __device__ __forceinline__ bool prefill_place(const PrefillParams& p, bool whole, int64_t x, int len, int add, int4& c) {
-    constexpr int64_t OV = STEP / 8 * kPlanStart;
+    const int64_t OV = STEP / 8 * p.plan_start;
     const int lane = threadIdx.x & 31;
     const int ctx = len - add, nt = prefill_tiles(add, p.tile_tokens);
     auto tile_sum = [&](int64_t j) { return j * (ctx + OV) + static_cast<int64_t>(p.tile_tokens) * (j * (j + 1) / 2); };
@@ -89,7 +86,7 @@ __device__ __forceinline__ bool prefill_place(const PrefillParams& p, bool whole
 template <int STEP, int THREADS>
 __device__ void prefill_plan(const PrefillParams& p, PlanScratch* s, int64_t* cum, int32_t* lens, int32_t* wide_of) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    constexpr int64_t OV = STEP / 8 * kPlanStart, CUT = STEP / 8 * kPlanCut;
+    const int64_t OV = STEP / 8 * p.plan_start, CUT = STEP / 8 * p.plan_cut;
     const int64_t S = p.shares;
     auto tile_sum = [&](int64_t ctx, int64_t j) { return j * (ctx + OV) + static_cast<int64_t>(p.tile_tokens) * (j * (j + 1) / 2); };
     auto warp_scan = [&](int64_t v) {
