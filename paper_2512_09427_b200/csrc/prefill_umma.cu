@@ -39,10 +39,11 @@ constexpr int kProducerWarp = kSoftmaxWarps, kMmaWarp = kSoftmaxWarps + 1;
 constexpr int kThreads = (kSoftmaxWarps + 2) * 32;
 constexpr int kMaxStages = 10;
 constexpr int kItemSlots = 4;
+constexpr int kPolyPairs = 3;
 constexpr float kRaiseAbove = 16.f, kTooLarge = 65536.f;         // how far a maximum, in log2, or a half step's sum of weights may pass the reference
 constexpr int kHalfBytes = 128 * 128;               // 64 elements of 128 rows: of a lane's queries, of a step's keys or values
 // barriers
-constexpr int kBarFull = 0, kBarEmpty = kMaxStages, kBarItem = 2 * kMaxStages, kBarQFull = kBarItem + kItemSlots,
+constexpr int kBarFull = 0, kBarEmpty = kMaxStages, kBarItem = 2 * kMaxStages, kBarRead = kBarItem + kItemSlots, kBarQFull = kBarRead + kItemSlots,
               kBarQFree = kBarQFull + 2, kBarS = kBarQFree + 2, kBarPa = kBarS + 2, kBarPb = kBarPa + 2, kBarHalf = kBarPb + 2,
               kBarO = kBarHalf + 2, kBarDrain = kBarO + 2, kNumBars = kBarDrain + 1;
 
@@ -77,14 +78,39 @@ __device__ __forceinline__ float row_max(const uint32_t (&s)[kChunk]) {
     return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
 }
 
-// Weights 2^(s * scale - ref) of a chunk, rounded to bf16, and their sum (unrounded).
+// 2^x on the fused multiply-add pipe, for x <= 127: x = n + f with |f| <= 1/2, 2^f by the polynomial of degree 4 with the
+// least relative error on that interval (2.6e-6, by Remez exchange), n added to the exponent.  Below 2^-126 the result is
+// some number below 2^-125; of a NaN it is the largest number or a NaN, so that the sum of weights is too large and
+// the caller takes the special-function unit instead.  Two at a time.
+__device__ __forceinline__ float2 poly_exp2(float2 x) {
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-126.f));
+    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-126.f));
+    const float2 round = make_float2(12582912.f, 12582912.f), back = make_float2(-12582912.f, -12582912.f);
+    const float2 t = add2(x, round), n = add2(t, back);
+    const float2 f = fma2(n, make_float2(-1.f, -1.f), x);
+    float2 y = fma2(f, make_float2(0.0095701f, 0.0095701f), make_float2(0.05591786f, 0.05591786f));
+    y = fma2(y, f, make_float2(0.24024745f, 0.24024745f));
+    y = fma2(y, f, make_float2(0.69312181f, 0.69312181f));
+    y = fma2(y, f, make_float2(0.99999926f, 0.99999926f));
+    return make_float2(__uint_as_float(__float_as_uint(y.x) + (__float_as_uint(t.x) << 23)),
+                       __uint_as_float(__float_as_uint(y.y) + (__float_as_uint(t.y) << 23)));
+}
+
+// Weights 2^(s * scale - ref) of a chunk, rounded to bf16, and their sum (unrounded).  POLY of its 16 pairs take the fused
+// multiply-add pipe, the others the special-function unit, which is the busier of the two: both lanes' weights alone keep
+// it for 2,048 of a step's 3,240 cycles (8 requests, chunks of 128 behind 1,920: 45.1 us with 0 pairs, 43.0 with 2, 42.0 with 3,
+// 42.8 with 4; one prompt of 16,384, where the card's power limit decides: the same with all of them).
+template <int POLY = 0>
 __device__ __forceinline__ float weights(const uint32_t (&s)[kChunk], float scale, float ref, uint32_t (&pk)[kChunk / 2]) {
     const float2 sc = make_float2(scale, scale), neg = make_float2(-ref, -ref);
     float2 sum[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
     for (int i = 0; i < kChunk / 2; ++i) {
         float2 x = fma2(make_float2(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1])), sc, neg);
-        x = make_float2(fast_exp2(x.x), fast_exp2(x.y));
+        if (i * POLY / 16 != (i + 1) * POLY / 16)
+            x = poly_exp2(x);
+        else
+            x = make_float2(fast_exp2(x.x), fast_exp2(x.y));
         sum[i & 1] = add2(sum[i & 1], x);
         pk[i] = pack_bf16(x.x, x.y);
     }
@@ -124,8 +150,8 @@ prefill_umma_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_con
     if (warp == kProducerWarp) {
         if (lane < 2) asm volatile("prefetch.tensormap [%0];" ::"l"(lane == 0 ? &kv_map : &q_map) : "memory");
         for (int i = lane; i < kNumBars; i += 32) {
-            const bool free = i == kBarQFree || i == kBarQFree + 1;          // a lane's softmax warps; and its last product
-            mbar_init(bar(i), free ? 5u : i >= kBarPa && i < kBarHalf ? 4u : 1u);
+            const bool read = i >= kBarRead && i < kBarQFull;        // all softmax warps; a lane's
+            mbar_init(bar(i), read ? kSoftmaxWarps : i >= kBarPa && i < kBarHalf ? 4u : 1u);
         }
         if (lane == 0) *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -184,13 +210,17 @@ prefill_umma_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_con
         bool more = walk.next(it);
         asm volatile("griddepcontrol.wait;" ::: "memory");               // 8-bit pools: the kernel ahead writes the rows
         while (ok) {
-            // The slot's last item lies four back, and both lanes' softmax warps have read the one two back (they arrive on
-            // kBarQFree when they have; the issuing warp is ahead of them).
-            PrefillItem* to = items + (n_items & (kItemSlots - 1));
+            // The slot's last item lies four back.  The softmax warps say when they have read it; the issuing warp has come to the
+            // one two back at least (kBarQFree).
+            const int slot = n_items & (kItemSlots - 1);
+            if (n_items >= kItemSlots)
+                ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar(kBarRead + slot), static_cast<uint32_t>(n_items / kItemSlots - 1) & 1u, abort_flag, p.status, limit));
+            if (!ok) break;
+            PrefillItem* to = items + slot;
             if (!more) it.t1 = 0;
             if (lane == 0) {
                 *to = it;
-                mbar_arrive(bar(kBarItem + (n_items & (kItemSlots - 1))));
+                mbar_arrive(bar(kBarItem + slot));
             }
             __syncwarp();
             if (!more) break;
@@ -405,7 +435,7 @@ prefill_umma_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_con
             const PrefillItem it = items[slot];
             if (it.t1 == 0) break;
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar(kBarQFree + L));          // the slot has been read
+            if (lane == 0) mbar_arrive(bar(kBarRead + slot));
             __syncwarp();
             const int own = lane_steps(it, L);
             const int tok = it.tok0 + L * lane_tokens + row_tok;
@@ -500,7 +530,7 @@ prefill_umma_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_con
                             const int c = 2 * half + k;
                             tmem_wait_row32(s[k]);
                             if (c < 3) tmem_ld_row32(t_s + static_cast<uint32_t>((c + 1) * kChunk), s[k ^ 1]);
-                            sum += weights(s[k], scale, ref, pk[k]);
+                            sum += weights<kPolyPairs>(s[k], scale, ref, pk[k]);
                         }
                         // no reference yet, or one that is too low (or a NaN, which stays)
                         if (__any_sync(0xFFFFFFFFu, m == -INFINITY || !(sum <= kTooLarge))) {

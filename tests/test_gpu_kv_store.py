@@ -116,3 +116,65 @@ def test_special_values(kind, fmt):
     top = a.unflatten(-1, (2, 32)).abs().amax(-1, keepdim=True).expand(-1, -1, 32).flatten(1)
     step = {"int8": top / 254, "int4": top / 14, "e4m3": a.abs() * 2.0 ** -4 + top / 448 * 2.0 ** -10}[fmt]
     assert ((a - b).abs() <= step * (1 + 2.0 ** -20) + a.abs() * 2.0 ** -21 + b.abs() * torch.finfo(s.io).eps / 2).all()
+
+
+def test_captured_and_on_a_side_stream():
+    s = SlabPool([64, 64], [33, 50], 2, 2, 64, "bf16")
+    t = SlabPool([64, 64], [0, 0], 2, 2, 64, "bf16")
+    st = Store(s, "int8", 64, 0, 2, 83)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        stream = torch.cuda.current_stream().cuda_stream
+        s.pool.pack_kv([0, 1], st.c, stream=stream)
+        t.pool.unpack_kv([1, 0], st.c, count=[33, 50], stream=stream)
+    for i in range(3):
+        for r in range(2):
+            for h in range(2):
+                at = s.base[r] * 2 + h * 64
+                s.mem[:, at:at + s.lens[r]] = torch.randn(4, s.lens[r], 64, generator=s.gen).to(s.io).cuda()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a in range(4):
+            for r in range(2):
+                x = slab_rows(s, a, r, 0, s.lens[r])
+                want = s.stored(restored(*quantised(x.float(), "int8", 64), "int8", 64), a)
+                assert torch.equal(slab_rows(t, a, 1 - r, 0, s.lens[r]), want), (i, a, r)
+
+
+def test_refusals():
+    odma = lib()
+    s = SlabPool([32, 48], [20, 40], 2, 2, 64, "bf16")
+    st = Store(s, "int8", 32, 0, 2, 60)
+    before = s.mem.clone()
+
+    def rc(unpack=False, reqs=(0, 1), first=None, count=None, n=None, **kw):
+        c = odma.KvStore(st.c.format, st.c.group, 0, 2, st.codes.data_ptr(), st.cb, st.scales.data_ptr(), st.sb)
+        for k, v in kw.items():
+            setattr(c, k, v)
+        ids = (ctypes.c_uint64 * len(reqs))(*reqs)
+        arr = lambda v: None if v is None else (ctypes.c_int32 * len(v))(*v)
+        f = odma._lib.odma_unpack_kv if unpack else odma._lib.odma_pack_kv
+        return f(s.pool._h, ids, arr(first), arr(count), len(reqs) if n is None else n, ctypes.byref(c), None)
+
+    for kw in ({"format": 4}, {"format": -1}, {"group": 0}, {"group": 24}, {"group": 128}, {"group": 8}, {"layer": -1}, {"layer": 1}, {"n_layers": 0},
+               {"n_layers": 3}, {"n_layers": 0x7FFFFFFF}, {"codes": None}, {"codes": st.codes.data_ptr() + 8}, {"codes_bytes": st.cb - 1},
+               {"scales": None}, {"scales": st.scales.data_ptr() + 2}, {"scales_bytes": st.sb - 1}, {"n": 0}, {"n": -1},
+               {"codes": s.mem.data_ptr()}, {"scales": s.mem.data_ptr() + 64}, {"codes": s.mem.data_ptr() - 16}, {"scales": st.codes.data_ptr() + 64},
+               {"first": [-1, 0]}, {"count": [-1, 0]}, {"first": [21, 0]}):
+        assert rc(**kw) == odma.ERR_INVALID, kw
+        if "first" not in kw:
+            assert rc(unpack=True, **{"count": [20, 40], **kw}) == odma.ERR_INVALID, kw
+    assert rc(unpack=True, first=[-1, 0], count=[1, 1]) == odma.ERR_INVALID
+    assert rc(reqs=(0, 7)) == odma.ERR_UNKNOWN_REQ and rc(unpack=True, reqs=(7, 0), count=[1, 1]) == odma.ERR_UNKNOWN_REQ
+    # beyond what is committed, beyond the slab; the same token twice
+    assert rc(count=[21, 1]) == odma.ERR_OVERFLOW and rc(first=[0, 40], count=[1, 1]) == odma.ERR_OVERFLOW
+    assert rc(unpack=True, count=[33, 1]) == odma.ERR_OVERFLOW
+    assert rc(first=[0x7FFFFFFF, 0], count=[1, 1]) == odma.ERR_OVERFLOW and rc(first=[0, 0], count=[0x7FFFFFFF, 1]) == odma.ERR_OVERFLOW
+    assert rc(unpack=True, reqs=(0, 0), first=[0, 4], count=[5, 5]) == odma.ERR_INVALID
+    torch.cuda.synchronize()
+    assert torch.equal(s.mem.view(torch.int16), before.view(torch.int16)) and (st.codes == 0x7F).all() and torch.isnan(st.scales).all()
+    # what may be asked for: nothing, the same request in two parts, a packed one several times
+    assert rc(count=[0, 0], codes=None, scales=None) == odma.OK and rc(first=[20, 40]) == odma.OK
+    assert rc(reqs=(0, 0, 1, 0), count=[20, 20, 0, 20]) == odma.OK
+    assert rc(unpack=True, reqs=(0, 0), first=[10, 0], count=[10, 10]) == odma.OK
+    assert s.sync() == 0
