@@ -8,7 +8,10 @@
 //
 // What bounds it: memory.  A thread takes 16 elements, 32 bytes of a bf16 row in one load and 16 or 8 bytes of codes in one
 // store, kUnits of them with all loads before the first store; the threads of a warp follow the store, where rows of a
-// token lie side by side, and meet whole rows of a slab.  A group's maximum goes through log2(G / 16) shuffles.
+// token lie side by side, and meet whole rows of a slab.  A group's maximum goes through log2(G / 16) shuffles.  12 requests
+// of 8,191 tokens in all, 28 layers of 4 heads of 128, bf16 <-> E4M3 (712 MB): out 119 us (6.0 TB/s), back 111 us (6.4 TB/s);
+// 5,001 tokens to 4 bits and back (753 MB): 129 us.  Out, the quantising counts too: 3 units of 128 threads 119 us, 2 or 4
+// of them 124 and 122, 4 of 256 127; two 16-byte loads per unit instead of one of 32 bytes 129.
 #include "device_utils.cuh"
 #include "odma.h"
 
@@ -17,8 +20,8 @@ namespace {
 
 using namespace dev;
 
-constexpr int kThreads = 256;
-constexpr int kUnits = 4;                            // units of 16 elements per thread
+constexpr int kThreads = 128;
+constexpr int kUnits = 3;                            // units of 16 elements per thread
 
 // Division by a number that all threads share: x / d = (x * m) >> (31 + s) for x below 2^31, with 2^s the first power of two that
 // reaches d and m = 2^(31 + s) / d rounded up: m d exceeds 2^(31 + s) by less than d, so the quotient is off by less than
@@ -40,6 +43,7 @@ template <int BYTES>
 struct Words {
     uint32_t w[BYTES / 4];
 };
+// Loads and stores of up to 32 bytes in one instruction: a warp's then meet whole sectors.  Nothing is read twice.
 __device__ __forceinline__ void load(const void* p, Words<16>& x) {
     const uint4 v = __ldcs(static_cast<const uint4*>(p));
     x.w[0] = v.x, x.w[1] = v.y, x.w[2] = v.z, x.w[3] = v.w;
@@ -48,27 +52,32 @@ __device__ __forceinline__ void load(const void* p, Words<8>& x) {
     const uint2 v = __ldcs(static_cast<const uint2*>(p));
     x.w[0] = v.x, x.w[1] = v.y;
 }
-__device__ __forceinline__ void load(const void* p, Words<32>& x) {
-    const uint4 a = __ldcs(static_cast<const uint4*>(p)), b = __ldcs(static_cast<const uint4*>(p) + 1);
-    x.w[0] = a.x, x.w[1] = a.y, x.w[2] = a.z, x.w[3] = a.w;
-    x.w[4] = b.x, x.w[5] = b.y, x.w[6] = b.z, x.w[7] = b.w;
+__device__ __forceinline__ void load8(const void* p, uint32_t* w) {
+    asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                 : "l"(p));
 }
+__device__ __forceinline__ void store8(void* p, const uint32_t* w) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
+                 "r"(w[5]), "r"(w[6]), "r"(w[7])
+                 : "memory");
+}
+__device__ __forceinline__ void load(const void* p, Words<32>& x) { load8(p, x.w); }
 __device__ __forceinline__ void load(const void* p, Words<64>& x) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint4 v = __ldcs(static_cast<const uint4*>(p) + i);
-        x.w[4 * i] = v.x, x.w[4 * i + 1] = v.y, x.w[4 * i + 2] = v.z, x.w[4 * i + 3] = v.w;
-    }
+    load8(p, x.w);
+    load8(static_cast<const uint8_t*>(p) + 32, x.w + 8);
 }
-template <int BYTES>
-__device__ __forceinline__ void store(void* p, const Words<BYTES>& x) {
-    if constexpr (BYTES == 8) {
-        __stcs(static_cast<uint2*>(p), make_uint2(x.w[0], x.w[1]));
-    } else {
-#pragma unroll
-        for (int i = 0; i < BYTES / 16; ++i)
-            __stcs(static_cast<uint4*>(p) + i, make_uint4(x.w[4 * i], x.w[4 * i + 1], x.w[4 * i + 2], x.w[4 * i + 3]));
-    }
+__device__ __forceinline__ void store(void* p, const Words<8>& x) { __stcs(static_cast<uint2*>(p), make_uint2(x.w[0], x.w[1])); }
+__device__ __forceinline__ void store(void* p, const Words<16>& x) { __stcs(static_cast<uint4*>(p), make_uint4(x.w[0], x.w[1], x.w[2], x.w[3])); }
+__device__ __forceinline__ void store(void* p, const Words<32>& x) { store8(p, x.w); }
+__device__ __forceinline__ void store(void* p, const Words<64>& x) {
+    store8(p, x.w);
+    store8(static_cast<uint8_t*>(p) + 32, x.w + 8);
+}
+
+// Pair i of f times `by`, each product rounded to fp32.
+__device__ __forceinline__ float2 times(const float (&f)[16], int i, float by) {
+    return mul2(make_float2(f[2 * i], f[2 * i + 1]), make_float2(by, by));
 }
 
 // ---- the pool's element types: 16 elements as floats, the bits of their largest magnitude
@@ -139,9 +148,10 @@ struct Elem<ODMA_DTYPE_FP8_E4M3> {
     }
     __device__ static void pack(const float (&f)[16], float inv, Words<16>& x) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            x.w[i] = pack_e4m3(__fmul_rn(f[4 * i], inv), __fmul_rn(f[4 * i + 1], inv)) |
-                     pack_e4m3(__fmul_rn(f[4 * i + 2], inv), __fmul_rn(f[4 * i + 3], inv)) << 16;
+        for (int i = 0; i < 4; ++i) {
+            const float2 a = times(f, 2 * i, inv), b = times(f, 2 * i + 1, inv);
+            x.w[i] = pack_e4m3(a.x, a.y) | pack_e4m3(b.x, b.y) << 16;
+        }
     }
 };
 
@@ -149,6 +159,9 @@ struct Elem<ODMA_DTYPE_FP8_E4M3> {
 
 constexpr float kMagic = 12582912.f;                 // 1.5 * 2^23: adding it rounds to the nearest whole number, ties to even,
                                                      // which then stands in the low bits
+// (one at a time: as a pair, the sum would be contracted with the product in front of it)
+__device__ __forceinline__ uint32_t rounded(float x, float magic) { return __float_as_uint(__fadd_rn(x, magic)); }
+
 template <int FORMAT>
 struct Format;
 template <>
@@ -166,10 +179,9 @@ struct Format<ODMA_STORE_INT8> {
     __device__ static void pack(const float (&f)[16], float inv, Words<16>& c) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            uint32_t b[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) b[k] = __float_as_uint(__fadd_rn(__fmul_rn(f[4 * i + k], inv), kMagic));
-            c.w[i] = __byte_perm(__byte_perm(b[0], b[1], 0x0040), __byte_perm(b[2], b[3], 0x0040), 0x5410);
+            const float2 a = times(f, 2 * i, inv), b = times(f, 2 * i + 1, inv);
+            c.w[i] = __byte_perm(__byte_perm(rounded(a.x, kMagic), rounded(a.y, kMagic), 0x0040),
+                                 __byte_perm(rounded(b.x, kMagic), rounded(b.y, kMagic), 0x0040), 0x5410);
         }
     }
     __device__ static void floats(const Words<16>& c, float scale, float (&f)[16]) {
@@ -185,13 +197,20 @@ template <>
 struct Format<ODMA_STORE_INT4> {
     static constexpr int kBytes = 8;
     static constexpr float kTop = 7.f;
+    // Numbers from 1 to 15 (8 more than meant), each with the constant bits of kMagic above it: shifted and added up, these
+    // make one constant, and flipping every nibble's first bit takes the 8 back.
     __device__ static void pack(const float (&f)[16], float inv, Words<8>& c) {
+        constexpr uint32_t kBits = 0x4B400000u, kAll = kBits * 0x11111111u;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             uint32_t w = 0;
 #pragma unroll
-            for (int k = 7; k >= 0; --k) w = w << 4 | (__float_as_uint(__fadd_rn(__fmul_rn(f[8 * i + k], inv), kMagic)) & 15u);
-            c.w[i] = w;
+            for (int k = 3; k >= 0; --k) {
+                const float2 a = times(f, 4 * i + k, inv);
+                w = (w << 4) + rounded(a.y, kMagic + 8.f);
+                w = (w << 4) + rounded(a.x, kMagic + 8.f);
+            }
+            c.w[i] = (w - kAll) ^ 0x88888888u;
         }
     }
     __device__ static void floats(const Words<8>& c, float scale, float (&f)[16]) {
@@ -203,36 +222,61 @@ struct Format<ODMA_STORE_INT4> {
     }
 };
 
-// Place of unit `u` of an array of the launch: unit of the store's array, offset in elements inside the pool's array.
-// `i` is the request of an earlier unit.
+// Units of an array of the launch, tokens in order: unit `in` of token `tok` is element 16 c of KV head `head`.  A block
+// takes kUnits runs of `step` tokens, a thread the same unit of each where a token has no more units than the block threads
+// (`step` is 0 where it has: every unit is worked out by itself).
 struct Place {
-    int64_t store, slab;
+    int64_t store, slab;                             // unit of the store's array, and of the pool's
 };
-__device__ __forceinline__ Place place(const StoreParams& p, uint32_t u, const Divider& per_token, const Divider& per_row, int unit, int& i) {
-    const uint32_t tok = quotient(u, per_token), in = u - tok * per_token.d, head = quotient(in, per_row), c = in - head * per_row.d;
-    while (static_cast<int>(tok) >= p.cu[i + 1]) ++i;
-    const int64_t row = p.row[i] + static_cast<int64_t>(head) * p.cap[i] + (static_cast<int>(tok) - p.cu[i]);
-    return Place{(static_cast<int64_t>(p.token0) * per_token.d) + u, (row * per_row.d + c) * unit};
-}
-// The request of the block's first unit.
-__device__ __forceinline__ int first_request(const StoreParams& p, uint32_t tok) {
-    int lo = 0, hi = p.n;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (p.cu[mid] <= static_cast<int>(tok)) lo = mid; else hi = mid;
+struct Run {
+    const StoreParams& p;
+    const Divider &per_token, &per_row;
+    uint32_t u0, units, stride, tok, in, head, c;
+    int i;                                           // the request of the last unit asked for
+    bool mine;
+
+    __device__ __forceinline__ Run(const StoreParams& params, const Divider& token, const Divider& row, uint32_t step)
+        : p(params), per_token(token), per_row(row) {
+        stride = step ? step * token.d : kThreads;
+        u0 = blockIdx.x * (stride * kUnits) + threadIdx.x;
+        units = static_cast<uint32_t>(p.cu[p.n]) * token.d;
+        mine = threadIdx.x < stride;
+        split(u0);
+        int lo = 0, hi = p.n;                        // the last request that begins at the token or in front of it
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (p.cu[mid] <= static_cast<int>(tok)) lo = mid; else hi = mid;
+        }
+        i = lo;
     }
-    return lo;
-}
+    __device__ __forceinline__ void split(uint32_t u) {
+        tok = quotient(u, per_token);
+        in = u - tok * per_token.d;
+        head = quotient(in, per_row);
+        c = in - head * per_row.d;
+    }
+    __device__ __forceinline__ bool has(int k) const { return mine && u0 + k * stride < units; }
+    __device__ __forceinline__ Place at(int k, uint32_t step) {
+        if (k > 0) {
+            if (step)
+                tok += step;
+            else
+                split(u0 + k * stride);
+        }
+        while (static_cast<int>(tok) >= p.cu[i + 1]) ++i;
+        const int64_t row = p.row[i] + static_cast<int64_t>(head) * p.cap[i] + (static_cast<int>(tok) - p.cu[i]);
+        return Place{static_cast<int64_t>(p.token0) * per_token.d + (u0 + k * stride), row * per_row.d + c};
+    }
+};
 
 template <int DTYPE, int FORMAT, bool PACK>
-__global__ void __launch_bounds__(kThreads) store_kernel(const __grid_constant__ StoreParams p, const Divider per_token, const Divider per_row) {
+__global__ void __launch_bounds__(kThreads) store_kernel(const __grid_constant__ StoreParams p, const __grid_constant__ Divider per_token,
+                                                        const __grid_constant__ Divider per_row, uint32_t step) {
     using E = Elem<DTYPE>;
     using F = Format<FORMAT>;
     constexpr int ES = E::kBytes / 16;               // bytes of an element
     const int a = blockIdx.y;
-    const uint32_t units = static_cast<uint32_t>(p.cu[p.n]) * per_token.d;
-    const uint32_t u0 = blockIdx.x * (kThreads * kUnits);
-    int i = first_request(p, quotient(u0, per_token));
+    Run run(p, per_token, per_row, step);
     uint8_t* pool = static_cast<uint8_t*>(p.pool) + (p.row0 + a * p.rows_per_array) * p.head_dim * ES;
     const int64_t array = static_cast<int64_t>(a) * p.store_tokens * per_token.d;
     uint8_t* codes = static_cast<uint8_t*>(p.codes) + array * F::kBytes;
@@ -246,12 +290,11 @@ __global__ void __launch_bounds__(kThreads) store_kernel(const __grid_constant__
     float scale[kUnits];
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
-        const uint32_t u = u0 + k * kThreads + threadIdx.x;
-        in[k] = u < units;
+        in[k] = run.has(k);
         if (!in[k]) continue;
-        at[k] = place(p, u, per_token, per_row, 16, i);
+        at[k] = run.at(k, step);
         if (PACK) {
-            load(pool + at[k].slab * ES, x[k]);
+            load(pool + at[k].slab * E::kBytes, x[k]);
         } else {
             load(codes + at[k].store * F::kBytes, c[k]);
             scale[k] = __ldg(scales + (at[k].store >> shift));
@@ -261,7 +304,8 @@ __global__ void __launch_bounds__(kThreads) store_kernel(const __grid_constant__
     for (int k = 0; k < kUnits; ++k) {
         float f[16];
         if (PACK) {
-            // (threads without a unit take part in the shuffles: units end with a row, so no group is shared with them)
+            // (threads without a unit take part in the shuffles; runs of units are whole tokens, or begin at a multiple of
+            // a warp's threads, so no group is shared with them)
             uint32_t top = in[k] ? E::top(x[k]) : 0u;
             for (int o = 1; o < lanes; o <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
             if (!in[k]) continue;
@@ -274,7 +318,7 @@ __global__ void __launch_bounds__(kThreads) store_kernel(const __grid_constant__
                 s = inv = 0.f;
             } else {
                 s = __fdiv_rn(most, F::kTop);
-                inv = __fdiv_rn(1.f, s);
+                inv = __frcp_rn(s);
             }
             E::floats(x[k], own.x, f);
             if (top >= E::kInf)
@@ -287,46 +331,45 @@ __global__ void __launch_bounds__(kThreads) store_kernel(const __grid_constant__
             if (!in[k]) continue;
             F::floats(c[k], scale[k], f);
             E::pack(f, own.y, x[k]);
-            store(pool + at[k].slab * ES, x[k]);
+            store(pool + at[k].slab * E::kBytes, x[k]);
         }
     }
 }
 
 // Rows as they are, in units of 16 bytes.
 template <bool PACK>
-__global__ void __launch_bounds__(kThreads) store_raw_kernel(const __grid_constant__ StoreParams p, const Divider per_token, const Divider per_row) {
+__global__ void __launch_bounds__(kThreads) store_raw_kernel(const __grid_constant__ StoreParams p, const __grid_constant__ Divider per_token,
+                                                            const __grid_constant__ Divider per_row, uint32_t step) {
     const int a = blockIdx.y;
-    const uint32_t units = static_cast<uint32_t>(p.cu[p.n]) * per_token.d, u0 = blockIdx.x * (kThreads * kUnits);
-    int i = first_request(p, quotient(u0, per_token));
+    Run run(p, per_token, per_row, step);
     uint4* pool = static_cast<uint4*>(p.pool) + (p.row0 + a * p.rows_per_array) * per_row.d;
     uint4* codes = static_cast<uint4*>(p.codes) + static_cast<int64_t>(a) * p.store_tokens * per_token.d;
     Place at[kUnits];
     uint4 x[kUnits];
 #pragma unroll
     for (int k = 0; k < kUnits; ++k) {
-        const uint32_t u = u0 + k * kThreads + threadIdx.x;
-        if (u >= units) continue;
-        at[k] = place(p, u, per_token, per_row, 1, i);
+        if (!run.has(k)) continue;
+        at[k] = run.at(k, step);
         x[k] = __ldcs(PACK ? pool + at[k].slab : codes + at[k].store);
     }
 #pragma unroll
     for (int k = 0; k < kUnits; ++k)
-        if (u0 + k * kThreads + threadIdx.x < units) __stcs(PACK ? codes + at[k].store : pool + at[k].slab, x[k]);
+        if (run.has(k)) __stcs(PACK ? codes + at[k].store : pool + at[k].slab, x[k]);
 }
 
 template <int DTYPE, int FORMAT>
-void launch_t(const StoreParams& p, dim3 grid, const Divider& per_token, const Divider& per_row, bool pack, cudaStream_t stream) {
+void launch_t(const StoreParams& p, dim3 grid, const Divider& per_token, const Divider& per_row, uint32_t step, bool pack, cudaStream_t stream) {
     if (pack)
-        store_kernel<DTYPE, FORMAT, true><<<grid, kThreads, 0, stream>>>(p, per_token, per_row);
+        store_kernel<DTYPE, FORMAT, true><<<grid, kThreads, 0, stream>>>(p, per_token, per_row, step);
     else
-        store_kernel<DTYPE, FORMAT, false><<<grid, kThreads, 0, stream>>>(p, per_token, per_row);
+        store_kernel<DTYPE, FORMAT, false><<<grid, kThreads, 0, stream>>>(p, per_token, per_row, step);
 }
 template <int DTYPE>
-cudaError_t launch_f(const StoreParams& p, int format, dim3 grid, const Divider& per_token, const Divider& per_row, bool pack, cudaStream_t stream) {
+cudaError_t launch_f(const StoreParams& p, int format, dim3 grid, const Divider& per_token, const Divider& per_row, uint32_t step, bool pack, cudaStream_t stream) {
     switch (format) {
-        case ODMA_STORE_E4M3: launch_t<DTYPE, ODMA_STORE_E4M3>(p, grid, per_token, per_row, pack, stream); break;
-        case ODMA_STORE_INT8: launch_t<DTYPE, ODMA_STORE_INT8>(p, grid, per_token, per_row, pack, stream); break;
-        case ODMA_STORE_INT4: launch_t<DTYPE, ODMA_STORE_INT4>(p, grid, per_token, per_row, pack, stream); break;
+        case ODMA_STORE_E4M3: launch_t<DTYPE, ODMA_STORE_E4M3>(p, grid, per_token, per_row, step, pack, stream); break;
+        case ODMA_STORE_INT8: launch_t<DTYPE, ODMA_STORE_INT8>(p, grid, per_token, per_row, step, pack, stream); break;
+        case ODMA_STORE_INT4: launch_t<DTYPE, ODMA_STORE_INT4>(p, grid, per_token, per_row, step, pack, stream); break;
         default: return cudaErrorInvalidValue;
     }
     return cudaGetLastError();
@@ -340,18 +383,20 @@ cudaError_t launch_store(const StoreParams& p, int format, int dtype, bool pack,
     const Divider per_row = divider(row), per_token = divider(row * p.kv_heads);
     const uint64_t units = static_cast<uint64_t>(p.cu[p.n]) * per_token.d;
     if (units == 0) return cudaSuccess;
-    const dim3 grid(static_cast<unsigned>((units + kThreads * kUnits - 1) / (kThreads * kUnits)), static_cast<unsigned>(p.arrays));
+    const uint32_t step = per_token.d <= kThreads ? kThreads / per_token.d : 0;
+    const uint64_t block = static_cast<uint64_t>(step ? step * per_token.d : kThreads) * kUnits;
+    const dim3 grid(static_cast<unsigned>((units + block - 1) / block), static_cast<unsigned>(p.arrays));
     if (format == ODMA_STORE_RAW) {
         if (pack)
-            store_raw_kernel<true><<<grid, kThreads, 0, stream>>>(p, per_token, per_row);
+            store_raw_kernel<true><<<grid, kThreads, 0, stream>>>(p, per_token, per_row, step);
         else
-            store_raw_kernel<false><<<grid, kThreads, 0, stream>>>(p, per_token, per_row);
+            store_raw_kernel<false><<<grid, kThreads, 0, stream>>>(p, per_token, per_row, step);
         return cudaGetLastError();
     }
     switch (dtype) {
-        case ODMA_DTYPE_F32: return launch_f<ODMA_DTYPE_F32>(p, format, grid, per_token, per_row, pack, stream);
-        case ODMA_DTYPE_BF16: return launch_f<ODMA_DTYPE_BF16>(p, format, grid, per_token, per_row, pack, stream);
-        case ODMA_DTYPE_FP8_E4M3: return launch_f<ODMA_DTYPE_FP8_E4M3>(p, format, grid, per_token, per_row, pack, stream);
+        case ODMA_DTYPE_F32: return launch_f<ODMA_DTYPE_F32>(p, format, grid, per_token, per_row, step, pack, stream);
+        case ODMA_DTYPE_BF16: return launch_f<ODMA_DTYPE_BF16>(p, format, grid, per_token, per_row, step, pack, stream);
+        case ODMA_DTYPE_FP8_E4M3: return launch_f<ODMA_DTYPE_FP8_E4M3>(p, format, grid, per_token, per_row, step, pack, stream);
     }
     return cudaErrorInvalidValue;
 }
