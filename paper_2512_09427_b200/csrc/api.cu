@@ -1369,7 +1369,7 @@ namespace {
 
 // The split and the workspace of a call of odma_prefill_attention.
 struct PrefillShape {
-    bool tensor = false;
+    bool tensor = false, queue = false;
     int32_t tile_tokens = 0, part_rows = 0, shares = 0, min_piece = 0, plan_start = 0, plan_cut = 0;
     int64_t wide_tokens = 0;                     // 8-bit pools: tokens widened
     uint64_t wide_bytes = 0, starts_bytes = 0, part_o_bytes = 0, part_ml_bytes = 0;
@@ -1395,6 +1395,8 @@ bool prefill_shape(const odma_pool* pool, int32_t q_heads, const odma_tables* t,
     w.part_rows = std::max(1, std::min(w.tile_tokens, t->n_new_total)) * group;
     w.shares = w.tensor ? pool->plan_ctas : prefill_plain_blocks() * pool->plan_ctas;
     w.min_piece = w.tensor ? prefill_min_piece(w.part_rows) : 1;
+    // no table of so many requests and new tokens has more tiles than this
+    w.queue = w.tensor && t->n <= kPrefillQueued && static_cast<int64_t>(t->n + t->n_new_total / w.tile_tokens) * pool->kv_heads > w.shares;
     w.plan_start = w.tensor ? kTensorStart : kPlainStart;
     w.plan_cut = w.tensor ? kTensorCut : kPlainCut;
     auto up = [](int64_t b) { return static_cast<uint64_t>((b + 255) / 256 * 256); };
@@ -1403,7 +1405,7 @@ bool prefill_shape(const odma_pool* pool, int32_t q_heads, const odma_tables* t,
         w.wide_tokens = built_on_device(t) ? pool->alloc.T() : std::min<int64_t>(pool->alloc.T(), t->kv_tokens + 15ll * t->n);
         w.wide_bytes = up(2 * w.wide_tokens * pool->kv_heads * D * 2);
     }
-    w.starts_bytes = up((w.shares + 1ll) * 16);
+    w.starts_bytes = up((w.shares + 1ll) * 16 + 4);
     w.part_o_bytes = up(2ll * w.shares * w.part_rows * D * 4);
     w.part_ml_bytes = up(2ll * w.shares * w.part_rows * 8);
     *out = w;
@@ -1457,6 +1459,7 @@ int32_t odma_prefill_attention(odma_pool* pool, int32_t layer, const void* q, in
     p.out = out;
     p.lse = lse;
     p.starts = reinterpret_cast<int4*>(at + w.wide_bytes);
+    if (w.queue) p.queue = reinterpret_cast<uint32_t*>(p.starts + w.shares + 1);
     p.part_o = reinterpret_cast<float*>(at + w.wide_bytes + w.starts_bytes);
     p.part_ml = reinterpret_cast<float*>(at + w.wide_bytes + w.starts_bytes + w.part_o_bytes);
     p.k_row0 = static_cast<int32_t>(2ll * layer * pool->rows_per_array);
@@ -1485,6 +1488,7 @@ int32_t odma_prefill_attention(odma_pool* pool, int32_t layer, const void* q, in
     pool->decode_was_last = false;
     pool->last_fused_tensor = false;
     cudaStream_t s = as_stream(stream);
+    if (p.queue && !fp8 && launch_prefill_begin(p, s) != cudaSuccess) return ODMA_ERR_CUDA;
     if (fp8) {
         p.wide = workspace;
         p.wide_tokens = w.wide_tokens;

@@ -231,6 +231,7 @@ struct PrefillParams {
     float* part_o;              // [2 shares][part_rows][head_dim] unnormalised
     float* part_ml;             // [2 shares][part_rows][2] reference (log2 domain) and sum
     int4* starts;               // [shares + 1] where each share begins: {request, KV head, tile, step}
+    uint32_t* queue;            // tiles taken from the common counter; null where the plan never uses one
     int32_t k_row0, v_row0;     // first row of the layer's K and V array
     int32_t n, n_new_total, q_heads, kv_heads, group, head_dim;
     int32_t tile_tokens;        // tokens of a tile of query rows (rows = tokens x group)
@@ -249,12 +250,14 @@ struct PrefillParams {
 constexpr int kMaxPrefillBatch = 4096;
 constexpr int kMaxPrefillGroup = 64;
 constexpr int kPrefillRows = 256;       // query rows of a tile on the tensor cores, in two lanes of half as many
+constexpr int kPrefillQueued = 32;      // requests up to which tiles may be taken from a common counter
 constexpr int kPrefillStep = 128;       // keys per step
 constexpr int kPrefillPlainRows = 64;   // and of the plain-ALU kernel
 constexpr int kPrefillPlainStep = 64;
 int32_t prefill_plain_blocks();         // blocks of the plain-ALU kernel that an SM holds
 cudaError_t launch_prefill_umma(const CUtensorMap& kv, const CUtensorMap& q, const PrefillParams& p, cudaStream_t stream);
 cudaError_t launch_prefill_plain(const PrefillParams& p, bool fp32, cudaStream_t stream);
+cudaError_t launch_prefill_begin(const PrefillParams& p, cudaStream_t stream);
 cudaError_t launch_prefill_widen(const PrefillParams& p, cudaStream_t stream);
 cudaError_t launch_prefill_merge(const PrefillParams& p, bool fp32, cudaStream_t stream);
 

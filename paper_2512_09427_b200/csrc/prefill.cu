@@ -59,8 +59,8 @@ __global__ void __launch_bounds__(kPlainThreads, 2) prefill_plain_kernel(const P
     const int tid = threadIdx.x, tx = tid & 15, ty = tid >> 4;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     int64_t* cum = reinterpret_cast<int64_t*>(smem_raw + sizeof(PlanScratch));
-    prefill_plan<kKeys, kPlainThreads>(p, &sm.plan, cum, reinterpret_cast<int32_t*>(cum + p.n), nullptr);
-    PrefillWalk<kKeys> walk(p, sm.plan);
+    prefill_plan<kKeys, kPlainThreads, false>(p, &sm.plan, cum, reinterpret_cast<int32_t*>(cum + p.n), nullptr);
+    PrefillWalk<kKeys, false> walk(p, sm.plan);
     const T* pool = static_cast<const T*>(p.pool);
     const T* Q = static_cast<const T*>(p.q);
     PrefillItem it;
@@ -205,12 +205,19 @@ cudaError_t launch_plain_t(const PrefillParams& p, cudaStream_t stream) {
 
 // ---- 8-bit pools
 
+// The counter that blocks take tiles from, for the kernel behind it, which is set up meanwhile.
+__global__ void prefill_begin_kernel(uint32_t* queue) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    *queue = 0u;
+}
+
 // Rows [0, len) of every head, K and V, of the requests with new tokens to the place that the plan gives them: blockIdx.y the
 // request, blockIdx.z the array and head; a thread takes kWiden vectors of 16 codes, all loads before the first store.
 constexpr int kWiden = 4;
 __global__ void __launch_bounds__(256) prefill_widen_kernel(const PrefillParams p) {
     __shared__ int64_t sums[8];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (p.queue && blockIdx.x + blockIdx.y + blockIdx.z + threadIdx.x == 0) *p.queue = 0u;
     const int i = blockIdx.y, len = __ldg(p.len + i), D = p.head_dim;
     if (prefill_new(p, i, len) == 0) return;
     int64_t before = 0;                              // tokens of the requests ahead
@@ -388,6 +395,11 @@ cudaError_t launch_prefill_plain(const PrefillParams& p, bool fp32, cudaStream_t
     if (p.head_dim == 32) return fp32 ? launch_plain_t<float, 32>(p, stream) : launch_plain_t<__nv_bfloat16, 32>(p, stream);
     if (!fp32) return cudaErrorInvalidValue;         // wider 16-bit rows: prefill_umma_kernel
     return p.head_dim == 64 ? launch_plain_t<float, 64>(p, stream) : p.head_dim == 128 ? launch_plain_t<float, 128>(p, stream) : cudaErrorInvalidValue;
+}
+
+cudaError_t launch_prefill_begin(const PrefillParams& p, cudaStream_t stream) {
+    prefill_begin_kernel<<<1, 1, 0, stream>>>(p.queue);
+    return cudaGetLastError();
 }
 
 cudaError_t launch_prefill_widen(const PrefillParams& p, cudaStream_t stream) {

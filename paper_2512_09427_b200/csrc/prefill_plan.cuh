@@ -11,6 +11,12 @@
 // A cut costs some steps too (its rows are written in 32 bits and read again), so when there are no more tiles than shares
 // and the longest tile ends before an equal share and a cut would, every share takes a tile; and a cut closer than
 // `min_piece` steps to an end of its tile moves to that end.
+//
+// Equal charges are not equal times: the SMs of one launch differ by a tenth (one prompt of 16,384 tokens: 2.22 M cycles on
+// average, 2.47 M on the slowest), and a cut costs time on both its sides.  So, with up to 32 requests, blocks take whole tiles
+// one by one from a common counter, requests with the longest slabs and their last tiles first, unless the tiles are so few
+// and long that the last ones would end a tenth and a cut later than equal shares.  (Prompts of 1,500 tokens: 32.8 us, by
+// equal shares 41.0; of 16,384: 1,379 and 1,532; 4,096 tokens behind 16,000, three tiles a block and 12 left over: 957 and 786.)
 #pragma once
 
 #include "device_utils.cuh"
@@ -23,6 +29,7 @@ struct alignas(16) PlanScratch {                // shared memory of one block
     int64_t total_cost, total_tiles;
     int4 cut[2];                    // where its share begins and ends: {request, KV head, tile, step}; n: behind everything
     int32_t longest, wide_at;       // wide_at: see PrefillItem, of the first
+    int32_t queued;                 // tiles are taken from the common counter (`cut` is behind everything)
 };
 
 __device__ __forceinline__ int prefill_tiles(int new_tokens, int tile_tokens) { return (new_tokens + tile_tokens - 1) / tile_tokens; }
@@ -82,8 +89,8 @@ __device__ __forceinline__ bool prefill_place(const PrefillParams& p, bool whole
 
 // Finds where this block's share begins and ends.  `cum` and `lens` [n] and, for an 8-bit pool, `wide_of` [n] are scratch.
 // Every thread of the block calls; a barrier is behind the last access.  Up to 32 requests the first two warps find a cut
-// each by themselves, with nothing but shuffles (one request: 1,300 cycles instead of 3,900); more go through the scratch.
-template <int STEP, int THREADS>
+// each by themselves, with nothing but shuffles (one request: 2,100 cycles instead of 3,900); more go through the scratch.
+template <int STEP, int THREADS, bool QUEUE>
 __device__ void prefill_plan(const PrefillParams& p, PlanScratch* s, int64_t* cum, int32_t* lens, int32_t* wide_of) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int64_t OV = STEP / 8 * p.plan_start, CUT = STEP / 8 * p.plan_cut;
@@ -129,7 +136,20 @@ __device__ void prefill_plan(const PrefillParams& p, PlanScratch* s, int64_t* cu
             const int64_t at = whole ? tiles_to - tiles : cost_to - cost, total = whole ? total_tiles : total_cost;
             const int64_t x = mine * share_cost(whole, total);
             int4 c = make_int4(p.n, 0, 0, 0);
-            if (x < total && mine != p.shares) {
+            bool queued = false;
+            if (QUEUE && p.queue && total_tiles > S) {
+                // Tiles one by one: with more than k S of them above a (k + 1)-th of a time, some block takes k + 1 and longer than that.
+                const float time = (1.1f * static_cast<float>(total_cost)) / static_cast<float>(S) + static_cast<float>(CUT);
+                const float first = static_cast<float>(len - add + OV), per_tile = 1.f / static_cast<float>(p.tile_tokens);
+                queued = true;
+#pragma unroll 1
+                for (int k = 0; k < 10; ++k) {
+                    const float below = fminf(fmaxf((time / (k + 1) - first) * per_tile, 0.f), static_cast<float>(nt));
+                    queued &= __reduce_add_sync(0xFFFFFFFFu, (nt - static_cast<int>(below)) * p.kv_heads) <= k * S;
+                }
+            }
+            if (warp == 0 && lane == 0) s->queued = queued;
+            if (!queued && x < total && mine != p.shares) {
                 const uint32_t some = __ballot_sync(0xFFFFFFFFu, add > 0);
                 // the last request with something to do whose cost before it is at most x
                 const int r = 31 - __clz(__ballot_sync(0xFFFFFFFFu, at <= x) & some);
@@ -149,6 +169,7 @@ __device__ void prefill_plan(const PrefillParams& p, PlanScratch* s, int64_t* cu
         __syncthreads();
         return;
     }
+    if (tid == 0) s->queued = 0;
     // a thread takes `per` requests in a row
     const int per = (p.n + THREADS - 1) / THREADS;
     int64_t cost = 0, tiles = 0, wide = 0;
@@ -241,16 +262,65 @@ struct PrefillItem {
     int wide_at;            // 8-bit pools: the request's first token in the widened rows
 };
 
-// Walks the items of a share.  Called by one whole warp (or by every thread, which then reads the same words).
-template <int STEP>
+// Walks the items of a share, or (QUEUE, and the plan says so) takes tiles from the common counter.  Called by one whole warp
+// (or by every thread, which then reads the same words).
+template <int STEP, bool QUEUE>
 struct PrefillWalk {
     const PrefillParams& p;
     int4 at, end;
     int len, add, ctx, cu, base, cap, wide_at;
+    // the counter's: lane r keeps the request with the r-th longest slab, and the tiles of all heads up to and with it
+    bool queued;
+    int request = 0, first_wide = 0, tiles_to = 0, taken = static_cast<int>(blockIdx.x);
 
     __device__ __forceinline__ PrefillWalk(const PrefillParams& params, const PlanScratch& s)
-        : p(params), at(s.cut[0]), end(s.cut[1]), wide_at(s.wide_at) {
+        : p(params), at(s.cut[0]), end(s.cut[1]), wide_at(s.wide_at), queued(QUEUE && s.queued) {
         if (at.x < p.n) fetch();
+    }
+    // One warp, before the first item, where `queued` is set.
+    __device__ __forceinline__ void sort() {
+        const int lane = threadIdx.x & 31;
+        const int mine = lane < p.n ? __ldg(p.len + lane) : 0, fresh = lane < p.n ? prefill_new(p, lane, mine) : 0;
+        auto sum_to = [&](auto v) {
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const auto x = __shfl_up_sync(0xFFFFFFFFu, v, o);
+                if (lane >= o) v += x;
+            }
+            return v;
+        };
+        const int64_t wide = fresh > 0 ? (mine + 15) & ~15 : 0, before = sum_to(wide) - wide;
+        first_wide = static_cast<int>(min(before, p.wide_tokens));
+        const int key = fresh > 0 ? mine : -1;
+        int rank = 0;
+#pragma unroll 1
+        for (int k = 0; k < 32; ++k) {
+            const int other = __shfl_sync(0xFFFFFFFFu, key, k);
+            rank += other > key || (other == key && k < lane);
+        }
+#pragma unroll 1
+        for (int k = 0; k < 32; ++k)
+            if (__shfl_sync(0xFFFFFFFFu, rank, k) == lane) request = k;
+        first_wide = __shfl_sync(0xFFFFFFFFu, first_wide, request);
+        tiles_to = sum_to(prefill_tiles(__shfl_sync(0xFFFFFFFFu, fresh, request), p.tile_tokens) * p.kv_heads);
+    }
+    // The next tile of the counter's: the first is the block's own number.
+    __device__ __forceinline__ bool take() {
+        if (taken < 0) {
+            if ((threadIdx.x & 31) == 0) taken = p.shares + static_cast<int>(atomicAdd(p.queue, 1u));
+            taken = __shfl_sync(0xFFFFFFFFu, taken, 0);
+        }
+        const uint32_t behind = __ballot_sync(0xFFFFFFFFu, tiles_to > taken);          // the first of these holds it
+        if (behind == 0) return false;
+        const int r = __ffs(behind) - 1, from = __shfl_sync(0xFFFFFFFFu, tiles_to, max(r - 1, 0));
+        at.x = __shfl_sync(0xFFFFFFFFu, request, r);
+        wide_at = __shfl_sync(0xFFFFFFFFu, first_wide, r);
+        fetch();
+        const int y = taken - (r > 0 ? from : 0), tile = y / p.kv_heads;
+        at.y = y - tile * p.kv_heads;
+        at.z = prefill_tiles(add, p.tile_tokens) - 1 - tile;
+        at.w = 0;
+        return true;
     }
     __device__ __forceinline__ void fetch() {
         len = __ldg(p.len + at.x);
@@ -261,6 +331,7 @@ struct PrefillWalk {
         cap = __ldg(p.cap + at.x);
     }
     __device__ __forceinline__ bool next(PrefillItem& it) {
+        if (QUEUE && queued && !take()) return false;
         if (at.x >= p.n || (at.x == end.x && at.y == end.y && at.z == end.z && at.w == end.w)) return false;
         const bool last = at.x == end.x && at.y == end.y && at.z == end.z;      // the share ends inside this tile
         const int tok0 = at.z * p.tile_tokens;
@@ -277,7 +348,9 @@ struct PrefillWalk {
         it.base = base;
         it.cap = cap;
         it.wide_at = wide_at;
-        if (last) {
+        if (QUEUE && queued) {
+            taken = -1;
+        } else if (last) {
             at = end;
         } else {
             at.w = 0;

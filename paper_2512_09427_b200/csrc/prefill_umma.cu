@@ -169,8 +169,8 @@ prefill_umma_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_con
     }
     int64_t* cum = reinterpret_cast<int64_t*>(kv + sizeof(PlanScratch));
     int32_t* lens = reinterpret_cast<int32_t*>(cum + p.n);
-    prefill_plan<kStep, kThreads>(p, plan, cum, lens, lens + p.n);
-    PrefillWalk<kStep> walk(p, *plan);
+    prefill_plan<kStep, kThreads, true>(p, plan, cum, lens, lens + p.n);
+    PrefillWalk<kStep, true> walk(p, *plan);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     fence_proxy_async();                             // the plan's words and the spare rows, before loads and products
     tc_fence_before();
@@ -207,8 +207,9 @@ prefill_umma_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_con
                 phase ^= 1u;
             }
         };
+        if (walk.queued) walk.sort();
         bool more = walk.next(it);
-        asm volatile("griddepcontrol.wait;" ::: "memory");               // 8-bit pools: the kernel ahead writes the rows
+        asm volatile("griddepcontrol.wait;" ::: "memory");               // the kernel ahead writes the counter and the rows of 8-bit pools
         while (ok) {
             // The slot's last item lies four back.  The softmax warps say when they have read it; the issuing warp has come to the
             // one two back at least (kBarQFree).
@@ -635,7 +636,7 @@ cudaError_t launch_t(const CUtensorMap& kv, const CUtensorMap& q, const PrefillP
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = p.wide ? 1 : 0;                    // behind prefill_widen_kernel: set up beside it
+    cfg.numAttrs = p.wide || p.queue ? 1 : 0;         // behind prefill_widen_kernel or prefill_begin_kernel: set up beside it
     return cudaLaunchKernelEx(&cfg, prefill_umma_kernel<D>, kv, q, p);
 }
 

@@ -68,6 +68,25 @@ def test_one_long_prompt(kind, q_heads, hkv, d):
     run_prefill(s, [0], [0], [new], q_heads, repeat=2)
 
 
+@pytest.mark.parametrize("kind,q_heads,hkv,d", [("bf16", 28, 4, 128), ("bf16", 12, 2, 64), ("e4m3", 8, 2, 128), ("f32", 4, 2, 64)])
+@pytest.mark.parametrize("ctas", [2, 5, 148])
+def test_more_tiles_than_blocks(kind, q_heads, hkv, d, ctas):
+    """Blocks take tiles in an order that differs from run to run; short and long slabs, requests without new tokens."""
+    r = random.Random(ctas)
+    new = [300, 0, 1, 90, 700, 33, 250, 2, 0, 129] + [r.randint(1, 60) for _ in range(21)] + [400]
+    ctx = [0, 4, 900, 513, 100, 0, 64, 0, 1, 250] + [r.choice([0, 40, 200]) for _ in range(21)] + [13]
+    s = pool_for(ctx, new, hkv, d, kind, seed=ctas, ctas=ctas, max_batch=32)
+    run_prefill(s, list(range(32)), ctx, new, q_heads, repeat=4)
+
+
+@pytest.mark.parametrize("kind,q_heads,hkv,d", [("bf16", 28, 4, 128), ("e4m3", 28, 4, 128)])
+@pytest.mark.parametrize("new,ctx", [([1500], [0]), ([1400], [4000]), ([2000, 18], [10, 3000]), ([1] * 30 + [1300, 0], [100] * 30 + [0, 7])])
+def test_tiles_of_even_and_uneven_length(kind, q_heads, hkv, d, new, ctx):
+    """Just more tiles than blocks: equal, rising, and one long one among short ones."""
+    s = pool_for(ctx, new, hkv, d, kind, seed=new[0], max_batch=32)
+    run_prefill(s, list(range(len(new))), ctx, new, q_heads, repeat=2)
+
+
 # ---- scores that leave their reference ---------------------------------------------------------------
 
 @pytest.mark.parametrize("kind,q_heads,hkv,d", [("bf16", 28, 4, 128), ("bf16", 12, 2, 64), ("f32", 2, 1, 64), ("e4m3", 8, 1, 128)])
@@ -223,6 +242,52 @@ def test_two_pools_on_two_streams():
     torch.cuda.synchronize()
     for (s, _, _, _, out, _), (w, _) in zip(pools, want):
         assert torch.equal(out, w) and s.sync() == 0
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+def test_two_calls_of_one_pool_at_once(kind):
+    """Two layers on two streams, with a workspace each, as captured graphs too; what a workspace held before does not matter."""
+    ctx, new = [100, 0, 7], [900, 400, 300]
+    s = pool_for(ctx, new, 4, 128, kind, seed=6, layers=2)
+    t = s.tables([0, 1, 2], new)
+    calls = []
+    for layer in range(2):
+        append_new(s, t, layer, new)
+        q = s.randn(sum(new), 28, 128)
+        want = call_prefill(s, layer, q, t)
+        ws = torch.full((s.pool.prefill_workspace_bytes(28, t),), 0xFF, dtype=torch.uint8, device="cuda")
+        calls.append((layer, q, want, ws, torch.empty_like(q), torch.empty(sum(new), 28, device="cuda"), torch.cuda.Stream()))
+
+    def run(c, stream):
+        s.pool.prefill_attention(c[0], c[1].data_ptr(), 28, t, c[3].data_ptr(), c[3].numel(), c[4].data_ptr(), c[5].data_ptr(), stream)
+
+    def check():
+        torch.cuda.synchronize()
+        for c in calls:
+            assert torch.equal(c[4], c[2][0]) and torch.equal(c[5], c[2][1])
+            c[4].zero_()
+            c[3].fill_(0xFF)
+        torch.cuda.synchronize()
+        assert s.sync() == 0
+
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for c in calls:
+            run(c, c[6].cuda_stream)
+    check()
+    graphs = []
+    for c in calls:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            run(c, torch.cuda.current_stream().cuda_stream)
+            run(c, torch.cuda.current_stream().cuda_stream)
+    for _ in range(3):
+        torch.cuda.synchronize()
+        for c, g in zip(calls, graphs):
+            with torch.cuda.stream(c[6]):
+                g.replay()
+                g.replay()
+        check()
 
 
 @pytest.mark.parametrize("kind,q_heads,hkv,d", [("bf16", 28, 4, 128), ("e4m3", 8, 2, 128), ("f32", 2, 1, 64)])
