@@ -15,13 +15,21 @@
 //
 // Warps 0-3 and 4-7: softmax of lane 0 and 1, a thread per row; warp 8: TMA producer; warp 9: issue of the products, QK(0) of
 // both lanes, then PV(u) QK(u + 1) of one and of the other for every step u, so S is only overwritten by a product issued
-// after the one that reads P from it; warp 10 does the issuing warp's waits for loads and hands stages back.
+// after the one that reads P from it.
 //
-// The softmax keeps a reference m per row, raised only when a maximum passes it by 2^8: P stays below 256, which bf16
-// relative to the fp32 accumulator does not mind.  So the weights need not wait for the maximum: both are found at once, with
-// the standing reference, for one half of a step and then the other, and where the reference turns out too low (in a tile's
-// first half step, and rarely later) the half is done again and sum and O are scaled.  P is rounded to bf16 for the product
-// (half a step: at most 2^-8 of a weight, random in sign over the keys); sums, maxima and O are fp32.
+// The softmax keeps a reference m per row, and no maximum is looked for while it stands: a half step's weights are taken
+// against it, and their sum, which is needed anyway, tells when it is too low (above 2^16; a NaN too).  Then the half is done
+// again with a new reference, and sum and O are scaled.  A tile's first step and the steps that a mask cuts look for their
+// maximum first.  bf16 and the fp32 sums have the range for weights above 1.  P is rounded to bf16 for the product (half a
+// step: at most 2^-8 of a weight, random in sign over the keys); sums, references and O are fp32.
+//
+// What bounds it: the tensor pipe, shared memory and the exponentials in turn.  A step's products want 2,048 cycles of the pipe
+// (256 x 128 x D twice), and the first product's operands as many of shared memory's; a lane's own chain, scores to weights to
+// products, is about 2,700, of which the other lane's covers what the pipe can take: 2,900 to 3,240 per step.  One prompt of
+// 16,384 tokens, 28 + 4 heads of 128: 1,378 us (1.40 PFLOP/s; tensor pipe 73 % busy before the tiles were dealt from a
+// counter), 1,604 back to back, at the card's power limit (1.2).  8 chunks of 128 tokens behind 1,920: 42.6 us (710 TFLOP/s).
+// A tile costs 4,000 cycles beside its steps (results 2,300: tensor memory to registers to rows; first loads and scores), the
+// launch about 7 us: set-up, plan, first loads, and the merge behind it.
 #include "odma.h"
 #include "prefill_plan.cuh"
 #include "tcgen05.cuh"
@@ -98,7 +106,7 @@ __device__ __forceinline__ float2 poly_exp2(float2 x) {
 
 // Weights 2^(s * scale - ref) of a chunk, rounded to bf16, and their sum (unrounded).  POLY of its 16 pairs take the fused
 // multiply-add pipe, the others the special-function unit, which is the busier of the two: both lanes' weights alone keep
-// it for 2,048 of a step's 3,240 cycles (8 requests, chunks of 128 behind 1,920: 45.1 us with 0 pairs, 43.0 with 2, 42.0 with 3,
+// it for 2,048 of a step's cycles (8 requests, chunks of 128 behind 1,920: 45.1 us with 0 pairs, 43.0 with 2, 42.0 with 3,
 // 42.8 with 4; one prompt of 16,384, where the card's power limit decides: the same with all of them).
 template <int POLY = 0>
 __device__ __forceinline__ float weights(const uint32_t (&s)[kChunk], float scale, float ref, uint32_t (&pk)[kChunk / 2]) {
@@ -428,6 +436,7 @@ prefill_umma_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_con
         const int row_tok = min(row / p.group, lane_tokens - 1), row_head = row % p.group;
         const uint32_t t_s = tmem + (static_cast<uint32_t>(warp & 3) << 21) + static_cast<uint32_t>(L) * 256u, t_o = t_s + 128u;
         const float scale = p.scale_log2;
+        const bool out_sectors = (reinterpret_cast<uintptr_t>(p.out) & 31u) == 0;        // (16 bytes are promised)
         uint32_t s_count = 0, o_count = 0;
         for (int n_items = 0; ok; ++n_items) {
             const int slot = n_items & (kItemSlots - 1);
@@ -591,8 +600,14 @@ prefill_umma_kernel(const __grid_constant__ CUtensorMap kv_map, const __grid_con
 #pragma unroll
                     for (int i = 0; i < 16; ++i) w[i] = pack_bf16(__uint_as_float(v[2 * i]) * inv, __uint_as_float(v[2 * i + 1]) * inv);
                     uint8_t* to = static_cast<uint8_t*>(p.out) + (out_row * D + 32 * c) * 2;
-                    store8(to, w);
-                    store8(to + 32, w + 8);
+                    if (out_sectors) {
+                        store8(to, w);
+                        store8(to + 32, w + 8);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            reinterpret_cast<uint4*>(to)[i] = make_uint4(w[4 * i], w[4 * i + 1], w[4 * i + 2], w[4 * i + 3]);
+                    }
                 }
                 __syncwarp();
             }

@@ -118,6 +118,27 @@ def test_special_values(kind, fmt):
     assert ((a - b).abs() <= step * (1 + 2.0 ** -20) + a.abs() * 2.0 ** -21 + b.abs() * torch.finfo(s.io).eps / 2).all()
 
 
+@pytest.mark.parametrize("kind,hkv,d", [("bf16", 3, 64), ("f32", 1, 128), ("e4m3", 2, 128), ("bf16", 1, 48)])
+@pytest.mark.parametrize("fmt", ["raw", "e4m3", "int8", "int4"])
+def test_sixteen_bytes_of_alignment(kind, hkv, d, fmt):
+    """Codes that begin 16 bytes behind a multiple of 32, scales 4 behind one of 16."""
+    odma = lib()
+    s = SlabPool([48, 32], [33, 21], 2, hkv, d, kind, seed=4)
+    st = check_pack(s, fmt, 16, [0, 1], None, None, 0, 2)
+    codes = torch.full((st.cb + 32,), 0xA5, dtype=torch.uint8, device="cuda")
+    scales = torch.full((st.sb // 4 + 2,), -7.0, device="cuda")
+    assert codes.data_ptr() % 32 == 0
+    c = odma.KvStore(st.c.format, 16, 0, 2, codes.data_ptr() + 16, st.cb, scales.data_ptr() + 4, st.sb)
+    s.pool.pack_kv([0, 1], c, stream=s.stream)
+    t = [SlabPool([48, 32], [0, 0], 2, hkv, d, kind) for _ in range(2)]
+    for pool, store in zip(t, (c, st.c)):
+        pool.pool.unpack_kv([0, 1], store, count=[33, 21], stream=s.stream)
+    assert s.sync() == 0
+    assert torch.equal(codes[16:-16], st.codes[:st.cb]) and (codes[:16] == 0xA5).all() and (codes[-16:] == 0xA5).all()
+    assert torch.equal(scales[1:-1], st.scales[:st.sb // 4]) and scales[0] == -7 and scales[-1] == -7
+    assert torch.equal(t[0].mem.view(torch.uint8), t[1].mem.view(torch.uint8))
+
+
 def test_captured_and_on_a_side_stream():
     s = SlabPool([64, 64], [33, 50], 2, 2, 64, "bf16")
     t = SlabPool([64, 64], [0, 0], 2, 2, 64, "bf16")

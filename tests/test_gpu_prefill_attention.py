@@ -303,6 +303,26 @@ def test_single_tokens_agree_with_decode(kind, q_heads, hkv, d):
     within(other, want, bound, "decode")
 
 
+@pytest.mark.parametrize("kind,q_heads,hkv,d", [("bf16", 28, 4, 128), ("bf16", 12, 2, 64), ("bf16", 6, 3, 32), ("f32", 2, 1, 64), ("e4m3", 8, 2, 128)])
+def test_sixteen_bytes_of_alignment(kind, q_heads, hkv, d):
+    """q and out begin 16 bytes behind a multiple of 32, lse 4 behind one of 16; whole tiles and cut ones."""
+    for ctx, new in (([5, 0], [40, 300]), ([2500], [30])):
+        s = pool_for(ctx, new, hkv, d, kind, seed=8)
+        t = s.tables(list(range(len(new))), new)
+        append_new(s, t, 0, new)
+        total, shift = sum(new), 16 // torch.empty(0, dtype=s.io).element_size()
+        q = s.randn(total * q_heads * d + shift, 1, 1).flatten()
+        out = torch.full((total * q_heads * d + 2 * shift,), -7.0, dtype=s.io, device="cuda")
+        lse = torch.full((total * q_heads + 2,), -7.0, device="cuda")
+        ws = torch.empty(s.pool.prefill_workspace_bytes(q_heads, t), dtype=torch.uint8, device="cuda")
+        assert q.data_ptr() % 32 == 0 and out.data_ptr() % 32 == 0
+        s.pool.prefill_attention(0, q.data_ptr() + 16, q_heads, t, ws.data_ptr(), ws.numel(), out.data_ptr() + 16, lse.data_ptr() + 4, s.stream)
+        assert s.sync() == 0
+        want = call_prefill(s, 0, q[shift:].view(total, q_heads, d).clone(), t)
+        assert torch.equal(out[shift:-shift], want[0].flatten()) and torch.equal(lse[1:-1], want[1].flatten())
+        assert (out[:shift] == -7).all() and (out[-shift:] == -7).all() and lse[0] == -7 and lse[-1] == -7
+
+
 def test_no_new_tokens_and_refusals():
     odma = lib()
     s = SlabPool([32, 32], [4, 9], 1, 2, 64, "bf16", max_batch=2, max_group=40)

@@ -24,6 +24,8 @@ def plan(p, new, ctx):
 
 
 def test_store_sizes():
+    # the header's struct: two pointers, two 64-bit sizes, four 32-bit numbers
+    assert ctypes.sizeof(odma.KvStore) == 48 and odma.KvStore.format.offset == 32 and odma.KvStore.n_layers.offset == 44
     p = pool()
     assert p.kv_store_bytes(odma.STORE_RAW, 0, 2, 10) == (2 * 2 * 10 * 4 * 256, 0)
     assert p.kv_store_bytes(odma.STORE_E4M3, 128, 1, 10) == (2 * 10 * 4 * 128, 2 * 10 * 4 * 4)
