@@ -373,7 +373,8 @@ int32_t odma_build_tables_device(odma_pool* pool, const int32_t* d_slabs, const 
  * [sum(n_new), q_heads, head_dim] (tokens in request order, then position order), computes
  *   out[t][h] = softmax_{k <= pos(t)}(q[t][h] . K[h div g][k] / sqrt(head_dim)) V[h div g].
  * The descriptor appends nothing (n_new_total = 0).  A slab is read once per new token, from
- * L2 after the first; packing several tokens of a chunk into one tensor-core tile is not done. */
+ * L2 after the first; odma_prefill_attention, which takes the step's own descriptor and not this one, puts
+ * the tokens of a chunk into one tensor-core tile. */
 int32_t odma_build_prefill_tables(odma_pool* pool, const uint64_t* reqs, const int32_t* n_new, int32_t n,
                                   void* d_table, uint64_t table_bytes, void* stream, odma_tables* out);
 
