@@ -390,7 +390,8 @@ int32_t odma_build_prefill_tables(odma_pool* pool, const uint64_t* reqs, const i
  * tokens before it in the same block of 128 keys NaN too (0 times it is not 0); a key row does not.
  * head_dim 32, 64 or 128, at most 64 query heads per KV head and 4,096 requests.
  * workspace: device, 256-byte aligned, the caller's: partial results of tiles that are cut between blocks and, for an
- * 8-bit pool, the batch's rows as bf16 (of a device-built table: as many as the pool holds).
+ * 8-bit pool, the batch's rows as bf16 (of a device-built table: as many as the pool holds; where a table of
+ * overlapping slabs names more, odma_check_status returns ODMA_ERR_OVERFLOW and the results mean nothing).
  * odma_prefill_workspace_bytes gives the size for a descriptor (0 for a bad shape); a larger one serves too.  Calls
  * that overlap on the GPU need one each.  May be captured; a captured call keeps an 8-bit pool's scales. */
 uint64_t odma_prefill_workspace_bytes(const odma_pool* pool, int32_t q_heads, const odma_tables* tables);

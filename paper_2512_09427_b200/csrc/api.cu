@@ -1401,8 +1401,9 @@ bool prefill_shape(const odma_pool* pool, int32_t q_heads, const odma_tables* t,
     w.plan_cut = w.tensor ? kTensorCut : kPlainCut;
     auto up = [](int64_t b) { return static_cast<uint64_t>((b + 255) / 256 * 256); };
     if (pool->dtype == ODMA_DTYPE_FP8_E4M3) {
-        // lengths rounded up to 16; on the device's own lengths all the pool can hold
-        w.wide_tokens = built_on_device(t) ? pool->alloc.T() : std::min<int64_t>(pool->alloc.T(), t->kv_tokens + 15ll * t->n);
+        // lengths rounded up to 16 (a request may be named more than once); on the device's own lengths all the pool can hold
+        w.wide_tokens = built_on_device(t) ? pool->alloc.T() : t->kv_tokens + 15ll * t->n;
+        if (t->kv_tokens < 0 || w.wide_tokens >= (int64_t(1) << 30) / pool->kv_heads) return false;      // rows count in 31 bits
         w.wide_bytes = up(2 * w.wide_tokens * pool->kv_heads * D * 2);
     }
     w.starts_bytes = up((w.shares + 1ll) * 16 + 4);

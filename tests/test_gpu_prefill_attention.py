@@ -244,6 +244,23 @@ def test_two_pools_on_two_streams():
         assert torch.equal(out, w) and s.sync() == 0
 
 
+@pytest.mark.parametrize("kind", ["bf16", "e4m3", "f32"])
+def test_a_request_named_several_times(kind):
+    """Its slab is read for each; together they are longer than the pool."""
+    s = pool_for([60], [20], 2, 128, kind, seed=1, max_batch=7)
+    first = s.tables([0], [20])
+    append_new(s, first, 0, [20])
+    q = s.randn(20, 8, 128)
+    want = call_prefill(s, 0, q, first)
+    t = s.tables([0] * 7, [20] * 7)
+    out, lse = call_prefill(s, 0, q.repeat(7, 1, 1), t)
+    ref = prefill_reference(s, 0, q, [0], [60], [20])
+    for i in range(7):                               # (cut at other places)
+        within(out[20 * i:20 * i + 20], ref[0], ref[2], "out")
+        within(lse[20 * i:20 * i + 20], ref[1], ref[3], "lse")
+    within(want[0], ref[0], ref[2], "out")
+
+
 @pytest.mark.parametrize("kind", ["bf16", "e4m3"])
 def test_two_calls_of_one_pool_at_once(kind):
     """Two layers on two streams, with a workspace each, as captured graphs too; what a workspace held before does not matter."""
