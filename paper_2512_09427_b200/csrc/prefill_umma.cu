@@ -86,28 +86,28 @@ __device__ __forceinline__ float row_max(const uint32_t (&s)[kChunk]) {
     return fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
 }
 
-// 2^x on the fused multiply-add pipe, for x <= 127: x = n + f with |f| <= 1/2, 2^f by the polynomial of degree 4 with the
-// least relative error on that interval (2.6e-6, by Remez exchange), n added to the exponent.  Below 2^-126 the result is
-// some number below 2^-125; of a NaN it is the largest number or a NaN, so that the sum of weights is too large and
-// the caller takes the special-function unit instead.  Two at a time.
+// 2^x on the fused multiply-add pipe: x = n + f with |f| <= 1/2, 2^f by the polynomial of degree 4 with the least relative
+// error on that interval (2.6e-6, by Remez exchange), times 2^n, whose exponent n + 127 is held to [0, 254] by one
+// instruction.  So below 2^-126 the result is 0, and above 2^127 it is one of that size and not what an exponent that has run into
+// the sign makes of it: the sum of weights is too large then and the caller takes the special-function unit instead, as it does
+// for infinities and NaN, which end as NaN, and for x below -2^23, where n's bits no longer mean n.  Two at a time.
 __device__ __forceinline__ float2 poly_exp2(float2 x) {
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.x) : "f"(-126.f));
-    asm("max.NaN.f32 %0, %0, %1;" : "+f"(x.y) : "f"(-126.f));
-    const float2 round = make_float2(12582912.f, 12582912.f), back = make_float2(-12582912.f, -12582912.f);
-    const float2 t = add2(x, round), n = add2(t, back);
+    constexpr float kRound = 12582912.f;             // 1.5 * 2^23: the sum's low bits are n (and 127 with it)
+    const float2 t = add2(x, make_float2(kRound + 127.f, kRound + 127.f)), n = add2(t, make_float2(-kRound - 127.f, -kRound - 127.f));
     const float2 f = fma2(n, make_float2(-1.f, -1.f), x);
     float2 y = fma2(f, make_float2(0.0095701f, 0.0095701f), make_float2(0.05591786f, 0.05591786f));
     y = fma2(y, f, make_float2(0.24024745f, 0.24024745f));
     y = fma2(y, f, make_float2(0.69312181f, 0.69312181f));
     y = fma2(y, f, make_float2(0.99999926f, 0.99999926f));
-    return make_float2(__uint_as_float(__float_as_uint(y.x) + (__float_as_uint(t.x) << 23)),
-                       __uint_as_float(__float_as_uint(y.y) + (__float_as_uint(t.y) << 23)));
+    auto power = [](float v) { return __int_as_float(__viaddmin_s32_relu(__float_as_int(v), -0x4B400000, 254) << 23); };
+    return mul2(y, make_float2(power(t.x), power(t.y)));
 }
 
 // Weights 2^(s * scale - ref) of a chunk, rounded to bf16, and their sum (unrounded).  POLY of its 16 pairs take the fused
 // multiply-add pipe, the others the special-function unit, which is the busier of the two: both lanes' weights alone keep
-// it for 2,048 of a step's cycles (8 requests, chunks of 128 behind 1,920: 45.1 us with 0 pairs, 43.0 with 2, 42.0 with 3,
-// 42.8 with 4; one prompt of 16,384, where the card's power limit decides: the same with all of them).
+// it for 2,048 of a step's cycles (8 requests, chunks of 128 behind 1,920, head_dim 128: 45.1 us with 0 pairs, 43.1 with 2, 43.0 with 3,
+// 43.0 with 4; 16 + 4 heads of 64: 46.8, 45.0, 43.3, 44.4; one prompt of 16,384 in a row, where the card's power limit decides: 1,717, 1,632,
+// 1,616, 1,604).
 template <int POLY = 0>
 __device__ __forceinline__ float weights(const uint32_t (&s)[kChunk], float scale, float ref, uint32_t (&pk)[kChunk / 2]) {
     const float2 sc = make_float2(scale, scale), neg = make_float2(-ref, -ref);
