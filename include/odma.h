@@ -183,7 +183,7 @@ typedef struct odma_tables {
     int32_t off_base, off_cap, off_len, off_cu_new, off_cta, off_items, off_combine;
     int32_t tile_tokens;
     int32_t one_new_each; /* 1 when every request appends exactly one token (decode step) */
-    int32_t reserved;     /* 1: built on the device (odma_build_tables_device) */
+    int32_t reserved;     /* 1: built on the device (odma_build_tables_device); 2: one stream per token (odma_build_prefill_tables) */
     int64_t kv_tokens; /* sum of len */
     uint64_t epoch;
 } odma_tables;
@@ -372,8 +372,8 @@ int32_t odma_build_tables_device(odma_pool* pool, const int32_t* d_slabs, const 
  * sum(n_new))); odma_decode_attention with the returned descriptor, q and out of shape
  * [sum(n_new), q_heads, head_dim] (tokens in request order, then position order), computes
  *   out[t][h] = softmax_{k <= pos(t)}(q[t][h] . K[h div g][k] / sqrt(head_dim)) V[h div g].
- * The descriptor appends nothing (n_new_total = 0).  A slab is read once per new token, from
- * L2 after the first; odma_prefill_attention, which takes the step's own descriptor and not this one, puts
+ * The descriptor appends nothing (n_new_total = 0, reserved = 2).  A slab is read once per new token, from
+ * L2 after the first; odma_prefill_attention, which takes the step's own descriptor and refuses this one, puts
  * the tokens of a chunk into one tensor-core tile. */
 int32_t odma_build_prefill_tables(odma_pool* pool, const uint64_t* reqs, const int32_t* n_new, int32_t n,
                                   void* d_table, uint64_t table_bytes, void* stream, odma_tables* out);
@@ -392,7 +392,7 @@ int32_t odma_build_prefill_tables(odma_pool* pool, const uint64_t* reqs, const i
  * workspace: device, 256-byte aligned, the caller's: partial results of tiles that are cut between blocks and, for an
  * 8-bit pool, the batch's rows as bf16 (of a device-built table: as many as the pool holds; where a table of
  * overlapping slabs names more, odma_check_status returns ODMA_ERR_OVERFLOW and the results mean nothing).
- * odma_prefill_workspace_bytes gives the size for a descriptor (0 for a bad shape); a larger one serves too.  Calls
+ * odma_prefill_workspace_bytes gives the size for a descriptor (0 for a bad one); a larger one serves too.  Calls
  * that overlap on the GPU need one each.  May be captured; a captured call keeps an 8-bit pool's scales. */
 uint64_t odma_prefill_workspace_bytes(const odma_pool* pool, int32_t q_heads, const odma_tables* tables);
 int32_t odma_prefill_attention(odma_pool* pool, int32_t layer, const void* q, int32_t q_heads, const odma_tables* tables,

@@ -327,8 +327,10 @@ bool rows_meet(const void* first, int64_t row, int64_t stride, int64_t rows, con
     return t < rows && t * stride < d + bytes;
 }
 
-// The table is written by a kernel (odma_build_tables_device); its counts in the descriptor are bounds.
-bool built_on_device(const odma_tables* t) { return t->reserved != 0; }
+// odma_tables.reserved: the table is written by a kernel (odma_build_tables_device) and its counts in the descriptor are bounds;
+// or it has a stream per new token (odma_build_prefill_tables), and says nothing of new tokens.
+constexpr int32_t kBuiltOnDevice = 1, kStreamPerToken = 2;
+bool built_on_device(const odma_tables* t) { return t->reserved == kBuiltOnDevice; }
 
 void fill_decode_params(const odma_pool* pool, int32_t layer, const void* q, int32_t q_heads,
                         const odma_tables* t, void* out, float* lse, DecodeParams* p) {
@@ -849,6 +851,7 @@ int32_t odma_build_prefill_tables(odma_pool* pool, const uint64_t* reqs, const i
     out->epoch = pool->alloc.epoch();
     out->n_new_total = 0;                            // nothing to append through this descriptor
     out->one_new_each = 0;
+    out->reserved = kStreamPerToken;
     if (cudaMemcpyAsync(d_table, st.host, static_cast<size_t>(out->words) * 4, cudaMemcpyHostToDevice,
                         as_stream(stream)) != cudaSuccess ||
         cudaEventRecord(st.done, as_stream(stream)) != cudaSuccess)
@@ -947,7 +950,7 @@ int32_t odma_build_tables_device(odma_pool* pool, const int32_t* d_slabs, const 
     t.words = t.off_combine + 4 * t.n_combine;
     t.tile_tokens = kTileTokens;
     t.one_new_each = d_n_new ? 0 : 1;
-    t.reserved = 1;                              // built_on_device
+    t.reserved = kBuiltOnDevice;
     t.kv_tokens = 0;
     t.epoch = pool->alloc.epoch();
     DeviceTablesParams p;
@@ -1387,6 +1390,7 @@ int32_t prefill_min_piece(int32_t rows) { return rows <= 32 ? 1 : rows <= 128 ? 
 bool prefill_shape(const odma_pool* pool, int32_t q_heads, const odma_tables* t, PrefillShape* out) {
     if (!pool || !t || t->n < 1 || t->n > kMaxPrefillBatch || t->n_new_total < 0 || q_heads < pool->kv_heads || q_heads % pool->kv_heads != 0)
         return false;
+    if (t->reserved == kStreamPerToken) return false;        // its requests are tokens
     const int32_t group = q_heads / pool->kv_heads, D = pool->head_dim;
     if (pool->plan_ctas > kMaxDeviceCtas || group > kMaxPrefillGroup || group > pool->alloc.config().max_group || (D != 32 && D != 64 && D != 128)) return false;
     PrefillShape w;
