@@ -382,8 +382,8 @@ int32_t odma_build_prefill_tables(odma_pool* pool, const uint64_t* reqs, const i
  * query heads of a KV head share every key, so a slab is read once per 256 rows (16- and 8-bit slabs of head_dim 64 and
  * 128, on the tensor cores; once per 64 rows in fp32 slabs and at head_dim 32) and not once per token.  tables: the step's
  * own descriptor (odma_build_tables with n_new, or odma_build_tables_device), the one its rows were appended with;
- * q, out: device, [n_new_total, q_heads, head_dim] in the pool's io type, 16-byte aligned, not overlapping; lse: device
- * fp32 [n_new_total, q_heads] or NULL.  With len[i] the tokens after the step and t the j-th of n_new[i] new ones,
+ * q, out: device, [n_new_total, q_heads, head_dim] in the pool's io type, 16-byte aligned; lse: device fp32 [n_new_total,
+ * q_heads] or NULL.  out, lse and the workspace must not overlap each other, q, the table or the pool (ODMA_ERR_INVALID).  With len[i] the tokens after the step and t the j-th of n_new[i] new ones,
  *   out[t][h] = softmax_{k <= len[i] - n_new[i] + j}(q[t][h] . K_i[h div g][k] / sqrt(head_dim)) V_i[h div g].
  * Softmax and accumulation are fp32; on the tensor cores the weights are rounded to bf16 for the second product.  Rows that
  * belong to no request (or a refused one) are left as they were.  A value row that is not finite makes the

@@ -1448,9 +1448,20 @@ int32_t odma_prefill_attention(odma_pool* pool, int32_t layer, const void* q, in
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || workspace_bytes < w.bytes()) return ODMA_ERR_INVALID;
     if ((reinterpret_cast<uintptr_t>(lse) & 3u) != 0) return ODMA_ERR_INVALID;
     const int32_t D = pool->head_dim;
-    // the queries are read while results are written: they must not meet
-    const int64_t row = static_cast<int64_t>(q_heads) * D * pool->io_bytes, all = row * tables->n_new_total;
-    if (rows_meet(q, all, all, 1, out, all)) return ODMA_ERR_INVALID;
+    // what is written meets nothing else that the call uses: all of it is read (and the workspace read again) meanwhile
+    const int64_t io = static_cast<int64_t>(tables->n_new_total) * q_heads * D * pool->io_bytes;
+    const struct {
+        const void* at;
+        int64_t bytes;
+    } parts[] = {{out, io},                          // written: these three
+                 {lse, static_cast<int64_t>(tables->n_new_total) * q_heads * 4},
+                 {workspace, static_cast<int64_t>(w.bytes())},
+                 {q, io},
+                 {pool->dev_base, 2ll * pool->layers * pool->rows_per_array * D * pool->elem_bytes},
+                 {tables->d_table, 4ll * tables->words}};
+    for (int i = 0; i < 3; ++i)
+        for (int k = i + 1; k < 6; ++k)
+            if (parts[k].at && rows_meet(parts[i].at, parts[i].bytes, parts[i].bytes, 1, parts[k].at, parts[k].bytes)) return ODMA_ERR_INVALID;
     DecodeParams d;
     fill_decode_params(pool, layer, q, q_heads, tables, out, lse, &d);
     PrefillParams p{};
