@@ -1397,7 +1397,7 @@ bool prefill_shape(const odma_pool* pool, int32_t q_heads, const odma_tables* t,
     w.tensor = pool->dtype != ODMA_DTYPE_F32 && D != 32;
     w.tile_tokens = w.tensor ? 2 * (kPrefillRows / 2 / group) : kPrefillPlainRows / group;
     w.part_rows = std::max(1, std::min(w.tile_tokens, t->n_new_total)) * group;
-    w.shares = w.tensor ? pool->plan_ctas : prefill_plain_blocks() * pool->plan_ctas;
+    w.shares = w.tensor ? pool->plan_ctas : prefill_plain_blocks(D) * pool->plan_ctas;
     w.min_piece = w.tensor ? prefill_min_piece(w.part_rows) : 1;
     // no table of so many requests and new tokens has more tiles than this
     w.queue = w.tensor && t->n <= kPrefillQueued && static_cast<int64_t>(t->n + t->n_new_total / w.tile_tokens) * pool->kv_heads > w.shares;

@@ -254,7 +254,7 @@ constexpr int kPrefillQueued = 32;      // requests up to which tiles may be tak
 constexpr int kPrefillStep = 128;       // keys per step
 constexpr int kPrefillPlainRows = 64;   // and of the plain-ALU kernel
 constexpr int kPrefillPlainStep = 64;
-int32_t prefill_plain_blocks();         // blocks of the plain-ALU kernel that an SM holds
+int32_t prefill_plain_blocks(int32_t head_dim);     // blocks of the plain-ALU kernel that an SM holds
 cudaError_t launch_prefill_umma(const CUtensorMap& kv, const CUtensorMap& q, const PrefillParams& p, cudaStream_t stream);
 cudaError_t launch_prefill_plain(const PrefillParams& p, bool fp32, cudaStream_t stream);
 cudaError_t launch_prefill_begin(const PrefillParams& p, cudaStream_t stream);

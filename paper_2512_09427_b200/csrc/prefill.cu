@@ -53,9 +53,15 @@ constexpr int plain_smem() {
     return rows > plan ? rows : plan;
 }
 static_assert(sizeof(PlanScratch) % 16 == 0, "rows of vectors lie behind it");
+// Blocks that an SM holds: two, where its 228 KB of shared memory have room for them and for the 1 KB that each takes beside its own (not at
+// head_dim 128, where a share per block more would be a second wave: 178 us instead of 168 for 1,024 tokens behind 2,000, 4 + 2 heads).
+template <int D>
+constexpr int plain_blocks() {
+    return 2 * (plain_smem<D>() + 1024) <= 228 * 1024 ? 2 : 1;
+}
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kPlainThreads, 2) prefill_plain_kernel(const PrefillParams p) {
+__global__ void __launch_bounds__(kPlainThreads, plain_blocks<D>()) prefill_plain_kernel(const PrefillParams p) {
     extern __shared__ __align__(16) uint8_t smem_raw[];
     PlainShared<D>& sm = *reinterpret_cast<PlainShared<D>*>(smem_raw);
     constexpr int OC = D / 16;                      // O columns of a thread: tx * CW + 16 * CW * c + e
@@ -395,7 +401,7 @@ cudaError_t launch_merge_t(const PrefillParams& p, cudaStream_t stream) {
 
 }  // namespace
 
-int32_t prefill_plain_blocks() { return 2; }
+int32_t prefill_plain_blocks(int32_t head_dim) { return head_dim == 32 ? plain_blocks<32>() : head_dim == 64 ? plain_blocks<64>() : plain_blocks<128>(); }
 
 cudaError_t launch_prefill_plain(const PrefillParams& p, bool fp32, cudaStream_t stream) {
     if (p.head_dim == 32) return fp32 ? launch_plain_t<float, 32>(p, stream) : launch_plain_t<__nv_bfloat16, 32>(p, stream);
