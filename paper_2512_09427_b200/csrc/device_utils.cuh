@@ -120,21 +120,6 @@ __device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_
 // async-proxy accesses (TMA, bulk copies, tcgen05.mma operands) that follow a synchronisation.
 __device__ __forceinline__ void fence_proxy_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// Barrier over `threads` threads; the second form tells whether any of them says yes.  Every thread comes to every
-// one of its barriers, also after a wait has given up.
-__device__ __forceinline__ void lane_sync(int id, int threads) {
-    asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
-}
-__device__ __forceinline__ bool lane_any(int id, int threads, bool yes) {
-    uint32_t any;
-    asm volatile(
-        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, %3, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
-        : "=r"(any)
-        : "r"(static_cast<uint32_t>(yes)), "r"(id), "r"(threads)
-        : "memory");
-    return any != 0;
-}
-
 __device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])

@@ -89,6 +89,21 @@ __device__ __forceinline__ float row_weights(const uint32_t (&s)[kCols], float s
     return (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
 }
 
+// Barrier over `threads` threads; the second form tells whether any of them says yes.  Every thread comes to every
+// one of its barriers, also after a wait has given up.
+__device__ __forceinline__ void lane_sync(int id, int threads) {
+    asm volatile("barrier.cta.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+__device__ __forceinline__ bool lane_any(int id, int threads, bool yes) {
+    uint32_t any;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbarrier.cta.red.or.pred q, %2, %3, p;\n\tselp.b32 %0, 1, 0, q;\n\t}"
+        : "=r"(any)
+        : "r"(static_cast<uint32_t>(yes)), "r"(id), "r"(threads)
+        : "memory");
+    return any != 0;
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 prefix_umma_kernel(const __grid_constant__ CUtensorMap map, const PrefixParams p) {
