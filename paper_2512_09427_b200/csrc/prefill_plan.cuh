@@ -252,7 +252,7 @@ __device__ void prefill_plan(const PrefillParams& p, PlanScratch* s, int64_t* cu
 
 // One piece of work: steps [t0, t1) of a tile.
 struct PrefillItem {
-    int request, head;
+    int head;
     int tok0;               // first token of the tile among the request's new ones
     int add, ctx;           // new tokens and tokens before them
     int cu;                 // the request's first row of q
@@ -336,7 +336,6 @@ struct PrefillWalk {
         const bool last = at.x == end.x && at.y == end.y && at.z == end.z;      // the share ends inside this tile
         const int tok0 = at.z * p.tile_tokens;
         const int steps = (ctx + min(tok0 + p.tile_tokens, add) + STEP - 1) / STEP;
-        it.request = at.x;
         it.head = at.y;
         it.tok0 = tok0;
         it.add = add;

@@ -64,6 +64,7 @@ struct Config {
     static constexpr int kRing = kStages * kStageBytes;
     static constexpr int kSmem = 2 * kQBytes + kRing + kItemSlots * static_cast<int>(sizeof(PrefillItem)) + kNumBars * 8 + 64 + 1024;
 };
+static_assert(kItemSlots * sizeof(PrefillItem) % 8 == 0, "barriers lie behind the items");
 static_assert(Config<128>::kSmem <= 232448 && Config<64>::kSmem <= 232448, "shared memory of a block");
 // the plan's scratch lies in the ring, before the first load
 static_assert(sizeof(PlanScratch) + kMaxPrefillBatch * 16 + 64 <= Config<128>::kRing, "room for the plan");
