@@ -270,10 +270,7 @@ __global__ void __launch_bounds__(256) prefill_widen_kernel(const PrefillParams 
                 o[2 * j] = pack_bf16(lo.x, lo.y);
                 o[2 * j + 1] = pack_bf16(hi.x, hi.y);
             }
-            uint4* to = dst + 2 * (v + u * step);
-            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]),
-                         "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7])
-                         : "memory");
+            store8(dst + 2 * (v + u * step), o);
         }
     }
 }

@@ -125,12 +125,6 @@ __device__ __forceinline__ float weights(const uint32_t (&s)[kChunk], float scal
     }
     return (sum[0].x + sum[0].y) + (sum[1].x + sum[1].y);
 }
-// 32 bytes, a whole sector, in one instruction.
-__device__ __forceinline__ void store8(void* p, const uint32_t* v) {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
-                 "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
-                 : "memory");
-}
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)

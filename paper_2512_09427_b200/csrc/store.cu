@@ -57,11 +57,6 @@ __device__ __forceinline__ void load8(const void* p, uint32_t* w) {
                  : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
                  : "l"(p));
 }
-__device__ __forceinline__ void store8(void* p, const uint32_t* w) {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
-                 "r"(w[5]), "r"(w[6]), "r"(w[7])
-                 : "memory");
-}
 __device__ __forceinline__ void load(const void* p, Words<32>& x) { load8(p, x.w); }
 __device__ __forceinline__ void load(const void* p, Words<64>& x) {
     load8(p, x.w);
