@@ -83,9 +83,10 @@ enum { ODMA_READOUT_AUTO = 0, ODMA_READOUT_LATE = 1, ODMA_READOUT_AT_ONCE = 2 };
 /* how odma_pack_kv holds an element (odma_kv_store.format) */
 enum { ODMA_STORE_RAW = 0, ODMA_STORE_E4M3 = 1, ODMA_STORE_INT8 = 2, ODMA_STORE_INT4 = 3 };
 
-/* kernels that odma_profile_read can report */
+/* kernels that odma_profile_read can report; PREFILL: every launch of odma_prefill_attention (an 8-bit pool's widening, the
+ * counter's reset and the merge of cut tiles among them), STORE: of odma_pack_kv and odma_unpack_kv */
 enum { ODMA_K_APPEND = 0, ODMA_K_DECODE = 1, ODMA_K_COMBINE = 2, ODMA_K_MIGRATE = 3,
-       ODMA_K_PROBE = 4, ODMA_K_COUNT = 5 };
+       ODMA_K_PROBE = 4, ODMA_K_PREFILL = 5, ODMA_K_STORE = 6, ODMA_K_COUNT = 7 };
 
 typedef struct odma_pool odma_pool;   /* opaque */
 typedef struct odma_paged odma_paged; /* opaque: a page-16 copy of the pool (ablation) */

@@ -678,7 +678,6 @@ int32_t store_impl(odma_pool* pool, const uint64_t* reqs, const int32_t* first, 
     if (most < 1) return ODMA_ERR_INVALID;
     pool->decode_was_last = false;
     pool->last_fused_tensor = false;
-    ProfScope ps(pool, ODMA_K_MIGRATE, as_stream(stream));
     for (int32_t l0 = 0; l0 < st->n_layers; l0 += kStoreLayers) {
         const int32_t layers = std::min(kStoreLayers, st->n_layers - l0);
         StoreParams p;
@@ -717,6 +716,7 @@ int32_t store_impl(odma_pool* pool, const uint64_t* reqs, const int32_t* first, 
                 }
             }
             token0 += p.cu[p.n];
+            ProfScope ps(pool, ODMA_K_STORE, as_stream(stream));
             if (launch_store(p, st->format, pool->dtype, pack, as_stream(stream)) != cudaSuccess) return ODMA_ERR_CUDA;
         }
     }
@@ -1504,21 +1504,25 @@ int32_t odma_prefill_attention(odma_pool* pool, int32_t layer, const void* q, in
     pool->decode_was_last = false;
     pool->last_fused_tensor = false;
     cudaStream_t s = as_stream(stream);
-    if (p.queue && !fp8 && launch_prefill_begin(p, s) != cudaSuccess) return ODMA_ERR_CUDA;
+    if (p.queue && !fp8) {
+        ProfScope ps(pool, ODMA_K_PREFILL, s);
+        if (launch_prefill_begin(p, s) != cudaSuccess) return ODMA_ERR_CUDA;
+    }
     if (fp8) {
         p.wide = workspace;
         p.wide_tokens = w.wide_tokens;
-        ProfScope ps(pool, ODMA_K_DECODE, s);
+        ProfScope ps(pool, ODMA_K_PREFILL, s);
         if (launch_prefill_widen(p, s) != cudaSuccess) return ODMA_ERR_CUDA;
         p.k_row0 = 0;
         p.v_row0 = static_cast<int32_t>(w.wide_tokens * pool->kv_heads);
     }
     {
-        ProfScope ps(pool, ODMA_K_DECODE, s);
+        ProfScope ps(pool, ODMA_K_PREFILL, s);
         const cudaError_t e = w.tensor ? launch_prefill_umma(fp8 ? wide_map : pool->maps.box[3], q_map, p, s) : launch_prefill_plain(p, fp32, s);
         if (e != cudaSuccess) return ODMA_ERR_CUDA;
     }
-    ProfScope ps(pool, ODMA_K_COMBINE, s);
+    if (p.shares < 2) return ODMA_OK;                // nothing is cut
+    ProfScope ps(pool, ODMA_K_PREFILL, s);
     return launch_prefill_merge(p, fp32, s) == cudaSuccess ? ODMA_OK : ODMA_ERR_CUDA;
 }
 

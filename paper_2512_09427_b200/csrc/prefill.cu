@@ -382,7 +382,6 @@ __global__ void __launch_bounds__(kMergeWarps * 32) prefill_merge_kernel(const P
 
 template <typename T, int V>
 cudaError_t launch_merge_t(const PrefillParams& p, cudaStream_t stream) {
-    if (p.shares < 2) return cudaSuccess;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(static_cast<unsigned>(std::min(4 * p.shares, (p.shares * p.part_rows + kMergeWarps - 1) / kMergeWarps)));
     cfg.blockDim = dim3(kMergeWarps * 32);

@@ -25,7 +25,7 @@ DTYPE_F32, DTYPE_BF16, DTYPE_FP8_E4M3 = 0, 1, 2
 DECODE_AUTO, DECODE_TCGEN05, DECODE_MMA_SYNC = 0, 1, 2
 READOUT_AUTO, READOUT_LATE, READOUT_AT_ONCE = 0, 1, 2
 STORE_RAW, STORE_E4M3, STORE_INT8, STORE_INT4 = 0, 1, 2, 3
-K_APPEND, K_DECODE, K_COMBINE, K_MIGRATE, K_PROBE = range(5)
+K_APPEND, K_DECODE, K_COMBINE, K_MIGRATE, K_PROBE, K_PREFILL, K_STORE = range(7)
 
 
 class Config(C.Structure):
