@@ -830,7 +830,8 @@ def run_config4(args):
 def run_prefill(args):
     """`--workload prefill`: a chunk of prompt tokens per request appended to Qwen-7B-shaped slabs and
     attended causally (odma_build_prefill_tables + the decode kernel: one stream per new token).  The
-    timed step is the chunk's attention on one layer; copies of the layer rotate so that L2 starts cold."""
+    timed step is the chunk's attention on one layer; copies of the layer rotate so that L2 starts cold.
+    `by_tiles`: the same chunk by tiles of query rows (odma_prefill_attention), timed the same way behind it."""
     if not torch.cuda.is_available():
         raise SystemExit("bench.py needs a CUDA device: the decode path has no CPU fallback")
     from paper_2512_09427_b200 import odma
@@ -865,24 +866,31 @@ def run_prefill(args):
     q = torch.stack([torch.cat([torch.stack([wl.q_rows(w.seed, layer, r, j, 28, 128, w.dtype, dev) for j in range(chunk)])
                                 for r in reqs]) for layer in range(copies)]).contiguous()
     out = torch.zeros_like(q)
+    ws = torch.empty(pool.prefill_workspace_bytes(28, t_app), dtype=torch.uint8, device=dev)
     def step(i):
         l = i % copies
         pool.decode_attention(l, q[l].data_ptr(), 28, pt, out[l].data_ptr(), 0, sd.stream)
-    for i in range(max(W, 3)):
-        step(i)
-    torch.cuda.synchronize()
-    clocks = ClockSampler(dev.index or 0)
-    ev = [torch.cuda.Event(enable_timing=True) for _ in range(6)]
-    t0 = time.time()
-    ev[0].record()
-    for r in range(5):
-        for i in range(K):
-            step(r * K + i)
-        ev[r + 1].record()
-    torch.cuda.synchronize()
-    clocks.mark(t0, time.time())
-    assert pool.check_status(sd.stream) == odma.OK
-    ms = statistics.median(ev[r].elapsed_time(ev[r + 1]) for r in range(5)) / K
+    def step_by_tiles(i):
+        l = i % copies
+        pool.prefill_attention(l, q[l].data_ptr(), 28, t_app, ws.data_ptr(), ws.numel(), out[l].data_ptr(), 0, sd.stream)
+    def timed(call, K):
+        for i in range(max(W, 3)):
+            call(i)
+        torch.cuda.synchronize()
+        clocks = ClockSampler(dev.index or 0)
+        ev = [torch.cuda.Event(enable_timing=True) for _ in range(6)]
+        t0 = time.time()
+        ev[0].record()
+        for r in range(5):
+            for i in range(K):
+                call(r * K + i)
+            ev[r + 1].record()
+        torch.cuda.synchronize()
+        clocks.mark(t0, time.time())
+        assert pool.check_status(sd.stream) == odma.OK
+        return statistics.median(ev[r].elapsed_time(ev[r + 1]) for r in range(5)) / K, clocks.stop()
+    ms, clocks = timed(step, K)
+    tiles_ms, tiles_clocks = timed(step_by_tiles, 8 * K)         # about as long
     keys = sum(ctx + j + 1 for j in range(chunk)) * n_req                 # (token, key) pairs per KV head
     flops = 2 * 2 * keys * 28 * 128                                      # two products, 28 query heads
     read_once = n_req * (ctx + chunk) * 2 * 4 * 128 * w.elem_bytes       # the slabs read once
@@ -900,7 +908,9 @@ def run_prefill(args):
                          "bytes_per_launch": read_per_token, "us_per_launch": ms * 1e3,
                          "note": "bytes = the slab prefix of every new token (this form streams it once per token, mostly from L2); "
                                  "the slabs themselves are " + str(read_once) + " bytes; tensor work " + str(flops) + " flop"},
-            "tflops": flops / (ms * 1e-3) / 1e12, "clocks": clocks.stop()}
+            "tflops": flops / (ms * 1e-3) / 1e12, "clocks": clocks,
+            "by_tiles": {"call": "odma_prefill_attention", "ms_per_step": tiles_ms, "value": n_req * chunk / (tiles_ms * 1e-3), "unit": UNIT,
+                         "tflops": flops / (tiles_ms * 1e-3) / 1e12, "clocks": tiles_clocks}}
     print(json.dumps(line), flush=True)
 
 
