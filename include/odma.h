@@ -383,10 +383,12 @@ int32_t odma_build_prefill_tables(odma_pool* pool, const uint64_t* reqs, const i
  * query heads of a KV head share every key, so a slab is read once per 256 rows (16- and 8-bit slabs of head_dim 64 and
  * 128, on the tensor cores; once per 64 rows in fp32 slabs and at head_dim 32) and not once per token.  tables: the step's
  * own descriptor (odma_build_tables with n_new, or odma_build_tables_device), the one its rows were appended with;
- * q, out: device, [n_new_total, q_heads, head_dim] in the pool's io type, 16-byte aligned; lse: device fp32 [n_new_total,
- * q_heads] or NULL.  out, lse and the workspace must not overlap each other, q, the table or the pool (ODMA_ERR_INVALID).  With len[i] the tokens after the step and t the j-th of n_new[i] new ones,
+ * q, out: device, [n_new_total, q_heads, head_dim] in the pool's io type, 16-byte aligned; lse: device
+ * fp32 [n_new_total, q_heads] or NULL.  out, lse and the workspace must not overlap each other, q, the table or the pool
+ * (ODMA_ERR_INVALID).  With len[i] the tokens after the step and t the j-th of n_new[i] new ones,
  *   out[t][h] = softmax_{k <= len[i] - n_new[i] + j}(q[t][h] . K_i[h div g][k] / sqrt(head_dim)) V_i[h div g].
- * Softmax and accumulation are fp32; on the tensor cores the weights are rounded to bf16 for the second product.  Rows that
+ * Scores, sums and results are fp32; on the tensor cores the weights are rounded to bf16 for the second product, and three of 16
+ * come from a polynomial good to 2.7e-6 of a weight (the others to 2e-7), which is as far as lse may be off beside its rounding.  Rows that
  * belong to no request (or a refused one) are left as they were.  A value row that is not finite makes the
  * tokens before it in the same block of 128 keys NaN too (0 times it is not 0); a key row does not.
  * head_dim 32, 64 or 128, at most 64 query heads per KV head and 4,096 requests.

@@ -9,7 +9,9 @@
 //  prefill_umma_kernel     tcgen05 tensor cores (prefill_umma.cu): 16- and 8-bit slabs, head_dim 64 and 128
 //  prefill_plain_kernel    plain ALUs, fp32 arithmetic: fp32 slabs, head_dim 32.  64 query rows and 64 keys in
 //                          shared memory, 4 x 4 scores and 4 rows of O per thread in registers.  Bound by shared memory's
-//                          reads beside the multiply-adds: 29 TFLOP/s (1,024 tokens behind 2,000, fp32, 4 + 2 heads of 128: 180 us)
+//                          reads beside the multiply-adds (8 vectors for 64 of them; larger tiles per thread would read less), and
+//                          nothing runs beside a step's loads: 30 TFLOP/s (1,024 tokens behind 2,000, fp32, 4 + 2 heads of 128: 168 to 173 us;
+//                          shared memory 65 % busy, the multiply-add pipe 50 %; heads of 64: 94 us, 68 and 50 %)
 //  prefill_widen_kernel    8-bit slabs: the codes of the requests with new tokens as bf16 (exact: a code has 4 significant
 //                          bits); the scales stay outside, in the score factor and in the result.  Bound by memory: 1 byte
 //                          in and 2 out per element, 31 MB of 30,510 tokens of 4 heads of 128 to 62 MB: 15.3 us cold (6.1 TB/s)

@@ -15,8 +15,10 @@
 // Equal charges are not equal times: the SMs of one launch differ by a tenth (one prompt of 16,384 tokens: 2.22 M cycles on
 // average, 2.47 M on the slowest), and a cut costs time on both its sides.  So, with up to 32 requests, blocks take whole tiles
 // one by one from a common counter, requests with the longest slabs and their last tiles first, unless the tiles are so few
-// and long that the last ones would end a tenth and a cut later than equal shares.  (Prompts of 1,500 tokens: 32.8 us, by
-// equal shares 41.0; of 16,384: 1,379 and 1,532; 4,096 tokens behind 16,000, three tiles a block and 12 left over: 957 and 786.)
+// and long that the last ones would end a tenth and a cut later than equal shares.  (In a row, prompts of
+// 1,500 tokens: 36 us, by equal shares 41; of 16,384: 1,647 and 1,769; 4,096 tokens behind 16,000, three tiles a block and 12 left
+// over: 1,003 and 919; 1,400 behind 30,000: 773 and 547.)  More requests keep equal shares: taking them 32 at a time made ragged
+// batches faster (64 of them 93 -> 85 us), but single tokens slower (512 of them 106 -> 121, one 14.3 -> 15.4).
 #pragma once
 
 #include "device_utils.cuh"

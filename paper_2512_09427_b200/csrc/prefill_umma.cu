@@ -26,8 +26,10 @@
 // What bounds it: the tensor pipe, shared memory and the exponentials in turn.  A step's products want 2,048 cycles of the pipe
 // (256 x 128 x D twice), and the first product's operands as many of shared memory's; a lane's own chain, scores to weights to
 // products, is about 2,700, of which the other lane's covers what the pipe can take: 2,900 to 3,240 per step.  One prompt of
-// 16,384 tokens, 28 + 4 heads of 128: 1,378 us (1.40 PFLOP/s, tensor pipe 73 % busy), 1,604
-// back to back, at the card's power limit (1.2).  8 chunks of 128 tokens behind 1,920: 42.6 us (710 TFLOP/s).
+// 16,384 tokens, 28 + 4 heads of 128: 1,400 to 1,480 us (1.35 PFLOP/s, tensor pipe 70 % busy), 1,605 to 1,650
+// back to back, at the card's power limit (1.2).  8 chunks of 128 tokens behind 1,920: 43.0 us (703 TFLOP/s).  With heads
+// of 64 the products want half as much and the lane's own chain is as long: a step still takes 3,000 cycles (4,096 tokens, 16 + 4
+// heads: 61 to 65 us, 530 to 560 TFLOP/s, tensor pipe 27 % busy, special-function unit 45 %).
 // A tile costs 4,000 cycles beside its steps (results 2,300: tensor memory to registers to rows; first loads and scores), the
 // launch about 7 us: set-up, plan, first loads, and the merge behind it.
 #include "odma.h"

@@ -10,7 +10,9 @@
 // store, kUnits of them with all loads before the first store; the threads of a warp follow the store, where rows of a
 // token lie side by side, and meet whole rows of a slab.  A group's maximum goes through log2(G / 16) shuffles.  12 requests
 // of 8,191 tokens in all, 28 layers of 4 heads of 128, bf16 <-> E4M3 (712 MB): out 119 us (6.0 TB/s), back 111 us (6.4 TB/s);
-// 5,001 tokens to 4 bits and back (753 MB): 129 us.  Out, the quantising counts too: 3 units of 128 threads 119 us, 2 or 4
+// 5,001 tokens to 4 bits and back (753 MB): 129 us; raw rows (939 MB) 143 us either way (6.55 TB/s).  8-bit pools move half as
+// much for as many conversions, and the issue slots fill up: 8,191 tokens out to 4 bits 127 us (3.0 TB/s, 87 % of the slots), to 8
+// bits 129 us (85 %), 8 bits back 100 us (75 %).  Out, the quantising counts too: 3 units of 128 threads 119 us, 2 or 4
 // of them 124 and 122, 4 of 256 127; two 16-byte loads per unit instead of one of 32 bytes 129.
 #include "device_utils.cuh"
 #include "odma.h"
